@@ -33,8 +33,10 @@
  *   halves the bytes decode and handoff move.  Entry points that take it:
  *   dopd_kv_write_fp8, dopd_decode_attn_fp8, dopd_decode_workspace_size,
  *   dopd_prefill_paged_attn_fp8 with its workspace size, dopd_pd_step_fp8
- *   with dopd_pd_step_workspace_size, and the handoff pack/unpack (byte
- *   copies); the others return DOPD_ERR_UNSUPPORTED for it.
+ *   with dopd_pd_step_workspace_size, dopd_window_attn_fp8 and
+ *   dopd_tree_attn_fp8 with their workspace sizes, and the handoff
+ *   pack/unpack, the page copies and the compaction (byte copies); the others
+ *   return DOPD_ERR_UNSUPPORTED for it.
  * - Fresh tokens are token-major: Q/out [T][Hq][d], K/V [T][Hkv][d].
  * - GQA: query head h uses KV head h / (Hq / Hkv); Hq % Hkv must be 0.
  * - Paged cache (one pool per layer, page_size = 16 tokens):
@@ -474,6 +476,158 @@ dopd_status dopd_pd_step_fp8(const dopd_attn_shape* shape, const void* q_dec,
 size_t dopd_pd_step_workspace_size(const dopd_attn_shape* shape,
                                    const int32_t* context_lens_host, int32_t num_dec,
                                    int32_t schedule);
+
+/*
+ * Windowed attention over the paged cache, with sinks.
+ * Paper: Eq. 1 over the KV-cache blocks (Sec. I, Sec. V-C) for layers that keep
+ * only a sliding window of each context and its first tokens: decode steps
+ * (Sec. IV-B, Eq. 12, whose bytes the window bounds) and chunks (Sec. III-A).
+ * As dopd_prefill_paged_attn (same row, cache and page-table arguments; a chunk
+ * of one token is a decode step), but a row at position p = prefix_lens[r] + i
+ * sees the cached positions
+ *     j <= p  with  j > p - window  or  j < num_sinks.
+ *   window >= 1 (1: the row's own position and the sinks), num_sinks >= 0.  A
+ *     window of at least every context gives dopd_prefill_paged_attn's result.
+ *   A page that no row of its request sees is not read: its page-table entry may
+ *     be stale or negative (its page freed).  K/V at positions a row does not see
+ *     never reach it, infinities and NaN included.
+ *   workspace: device memory of at least dopd_window_workspace_size() bytes for
+ *     the same arguments, 256-byte aligned, any contents; it holds the partial
+ *     results of items whose keys are split over several workgroups (merged
+ *     exactly, by log-sum-exp rescaling, on the same stream).  May be null when
+ *     that needs none.  Calls that overlap in time must not share it.
+ *   lse (nullable): fp32 [T][Hq].
+ * Requests of at most 16 rows times Hq / Hkv run one kernel, the others another;
+ * a call that holds both launches both.  Any Hq / Hkv.  q, out and the pools are
+ * 16-byte aligned, prefix_lens[r] + n_r is at most 2^30, and
+ * n_r * (Hq / Hkv)^2 < 2^32 (DOPD_ERR_INVALID_SHAPE otherwise).
+ * bf16: products of bf16 operands with fp32 accumulation, weights rounded to bf16
+ * before the product with V; the row sums (and lse) hold the unrounded weights.
+ * fp32: fp32 throughout.
+ */
+dopd_status dopd_window_attn(const dopd_attn_shape* shape, const void* q, const void* k_pool,
+                             const void* v_pool, int32_t num_pages, const int32_t* page_table,
+                             int32_t page_table_stride, const int32_t* cu_seqlens,
+                             const int32_t* cu_seqlens_host, const int32_t* prefix_lens,
+                             const int32_t* prefix_lens_host, int32_t num_reqs, int32_t window,
+                             int32_t num_sinks, void* out, float* lse, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/*
+ * Windowed attention over E4M3 pools.
+ * Paper: as dopd_window_attn (Eq. 1, Sec. I, Sec. IV-B) over FP8 blocks
+ * (Sec. VI-A).
+ * shape->dtype = DOPD_FP8_E4M3: dopd_window_attn's operation with
+ * K_j = code * k_scale[c] and V_j = code * v_scale[c] for KV head c (scales as in
+ * dopd_prefill_paged_attn_fp8); q and out bf16.
+ */
+dopd_status dopd_window_attn_fp8(const dopd_attn_shape* shape, const void* q, const void* k_pool,
+                                 const void* v_pool, const float* k_scale, const float* v_scale,
+                                 int32_t num_pages, const int32_t* page_table,
+                                 int32_t page_table_stride, const int32_t* cu_seqlens,
+                                 const int32_t* cu_seqlens_host, const int32_t* prefix_lens,
+                                 const int32_t* prefix_lens_host, int32_t num_reqs,
+                                 int32_t window, int32_t num_sinks, void* out, float* lse,
+                                 void* workspace, size_t workspace_bytes, void* stream);
+
+/* Workspace bytes dopd_window_attn(_fp8) needs for these arguments on the current
+ * device (at least 256; 0 on bad input).
+ * Paper: as dopd_window_attn (Eq. 1, Sec. I); the partial results are an exact
+ * rewrite of the softmax of Eq. 1. */
+size_t dopd_window_workspace_size(const dopd_attn_shape* shape, const int32_t* cu_seqlens_host,
+                                  const int32_t* prefix_lens_host, int32_t num_reqs,
+                                  int32_t window, int32_t num_sinks);
+
+/*
+ * Attention of a tree of drafted tokens over the paged cache.
+ * Paper: Eq. 1 over the KV-cache blocks (Sec. I, Sec. V-C) for a decode step
+ * (Sec. IV-B) that verifies several drafted tokens of each request at once, each
+ * cached byte of Eq. 12 read once for all of them.
+ * Request r has prefix_lens[r] cached tokens and n_r drafts, rows cu_seqlens[r] ..
+ * of q/out [T][Hq][d], whose K/V are already in the pools at positions
+ * prefix_lens[r] .. prefix_lens[r] + n_r - 1 (dopd_kv_write with start_pos =
+ * prefix_lens).  Draft i sees every position before prefix_lens[r], and draft j of
+ * its request where bit j % 32 of
+ *     tree_mask[(cu_seqlens[r] + i) * mask_words + j / 32]
+ * is set (a tree: itself and its ancestors; any mask is allowed, bits from n_r on
+ * are ignored).  tree_mask: device uint32 [T][mask_words], 1 <= mask_words <= 32,
+ * n_r <= 32 * mask_words.
+ *   A row that sees nothing (no cached token, an empty mask) has out = 0 and lse =
+ *   -inf.  With the mask of a chain this is dopd_prefill_paged_attn; a single
+ *   draft is a decode step with context_lens = prefix_lens + 1.
+ * Other arguments, workspace (dopd_tree_workspace_size), limits, rounding and the
+ * treatment of what a row does not see as in dopd_window_attn.
+ */
+dopd_status dopd_tree_attn(const dopd_attn_shape* shape, const void* q, const void* k_pool,
+                           const void* v_pool, int32_t num_pages, const int32_t* page_table,
+                           int32_t page_table_stride, const int32_t* cu_seqlens,
+                           const int32_t* cu_seqlens_host, const int32_t* prefix_lens,
+                           const int32_t* prefix_lens_host, int32_t num_reqs,
+                           const uint32_t* tree_mask, int32_t mask_words, void* out, float* lse,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Tree attention over E4M3 pools.
+ * Paper: as dopd_tree_attn (Eq. 1, Sec. IV-B, Eq. 12) over FP8 blocks (Sec. VI-A).
+ * shape->dtype = DOPD_FP8_E4M3: dopd_tree_attn's operation with K_j = code *
+ * k_scale[c] and V_j = code * v_scale[c] for KV head c; q and out bf16.
+ */
+dopd_status dopd_tree_attn_fp8(const dopd_attn_shape* shape, const void* q, const void* k_pool,
+                               const void* v_pool, const float* k_scale, const float* v_scale,
+                               int32_t num_pages, const int32_t* page_table,
+                               int32_t page_table_stride, const int32_t* cu_seqlens,
+                               const int32_t* cu_seqlens_host, const int32_t* prefix_lens,
+                               const int32_t* prefix_lens_host, int32_t num_reqs,
+                               const uint32_t* tree_mask, int32_t mask_words, void* out,
+                               float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Workspace bytes dopd_tree_attn(_fp8) needs for these arguments on the current
+ * device (at least 256; 0 on bad input).
+ * Paper: as dopd_tree_attn (Eq. 1, Sec. IV-B); the partial results are an exact
+ * rewrite of the softmax of Eq. 1. */
+size_t dopd_tree_workspace_size(const dopd_attn_shape* shape, const int32_t* cu_seqlens_host,
+                                const int32_t* prefix_lens_host, int32_t num_reqs);
+
+/*
+ * Moves accepted drafts to the places behind their prefix, in every layer.
+ * Paper: the KV-cache blocks kept per request (Sec. I, Sec. II-C), whose capacity
+ * bounds a D-instance's batch (Sec. IV-D, Eq. 11): rejected drafts leave no holes.
+ * Request r takes num_accepted[r] drafts: position prefix_lens[r] + i receives the
+ * K and V that position prefix_lens[r] + accepted[r * max_accepted + i] held before
+ * the call, for i < num_accepted[r].  A row of accepted is strictly increasing (a
+ * path of a tree whose drafts come after their parents), so accepted[i] >= i.  Pure
+ * bit copy in place; every other slot is left untouched (what the drafts held
+ * behind the accepted ones stays, dead).
+ *   k_pool/v_pool: with a leading layer dimension, as in dopd_kv_pack_for_handoff;
+ *     requests do not share the pages that are written (dopd_kv_copy_pages first).
+ *   prefix_lens, accepted [num_reqs][max_accepted], num_accepted [num_reqs] are
+ *     device arrays (what a step accepts need not reach the host): a count above
+ *     max_accepted is taken as max_accepted, a negative one as 0; a move whose
+ *     positions lie outside the page table or whose pages lie outside
+ *     [0, num_pages), or with accepted[i] < i, is left out.
+ * All three dtypes.  Pools are 16-byte aligned.
+ */
+dopd_status dopd_kv_compact(const dopd_attn_shape* shape, int32_t num_layers, void* k_pool,
+                            void* v_pool, int32_t num_pages, const int32_t* page_table,
+                            int32_t page_table_stride, const int32_t* prefix_lens,
+                            const int32_t* accepted, const int32_t* num_accepted,
+                            int32_t max_accepted, int32_t num_reqs, void* stream);
+
+/*
+ * Copies whole pages to other pages of the same pools, in every layer.
+ * Paper: the KV-cache blocks and their fragmentation (Sec. II-C, Sec. V-C): a
+ * request that forks copies the block it goes on writing and shares the others
+ * through its page table; scattered blocks are moved together.
+ * Page dst_pages[i] of every layer's K and V pool receives page src_pages[i],
+ * i < num_copies.  Pages of dst_pages are distinct and none is in src_pages; a
+ * source may be copied to several.  src_pages/dst_pages: device int32; an entry
+ * with an id outside [0, num_pages) is left out (lists of a fixed size may be
+ * padded with -1).  Pure bit copy.  k_pool/v_pool: with a leading layer dimension.
+ * All three dtypes.  Pools are 16-byte aligned.
+ */
+dopd_status dopd_kv_copy_pages(const dopd_attn_shape* shape, int32_t num_layers, void* k_pool,
+                               void* v_pool, int32_t num_pages, const int32_t* src_pages,
+                               const int32_t* dst_pages, int32_t num_copies, void* stream);
 
 /*
  * Handoff pack of prefill-completed requests.

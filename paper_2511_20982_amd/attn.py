@@ -36,6 +36,9 @@ EXPORTS = (
     "dopd_kv_pack_for_handoff", "dopd_kv_unpack_from_handoff", "dopd_validate_page_table_host",
     "dopd_kv_write_pack_for_handoff", "dopd_pd_step", "dopd_pd_step_fp8",
     "dopd_pd_step_workspace_size",
+    "dopd_window_attn", "dopd_window_attn_fp8", "dopd_window_workspace_size",
+    "dopd_tree_attn", "dopd_tree_attn_fp8", "dopd_tree_workspace_size",
+    "dopd_kv_copy_pages", "dopd_kv_compact",
     "dopd_status_string",
     "dopd_last_hip_error",
 )
@@ -83,6 +86,12 @@ LAUNCHES = {
     "dopd_kv_write_pack_for_handoff": "sddddididhiddp",
     "dopd_pd_step": "sdddhiddddddhidddddiiddidzp",
     "dopd_pd_step_fp8": "sdddhiddddddhidddddddiiddidzp",
+    "dopd_window_attn": "sdddididhdhiiidddzp",
+    "dopd_window_attn_fp8": "sdddddididhdhiiidddzp",
+    "dopd_tree_attn": "sdddididhdhididddzp",
+    "dopd_tree_attn_fp8": "sdddddididhdhididddzp",
+    "dopd_kv_copy_pages": "siddiddip",
+    "dopd_kv_compact": "siddididddiip",
 }
 
 _LIB = None
@@ -108,7 +117,9 @@ def lib():
                         ("dopd_prefill_paged_workspace_size", [SP, P, P, i32, i32]),
                         ("dopd_prefill_paged_fp8_workspace_size", [SP, P, P, i32, i32]),
                         ("dopd_decode_workspace_size", [SP, P, i32, i32]),
-                        ("dopd_pd_step_workspace_size", [SP, P, i32, i32])):
+                        ("dopd_pd_step_workspace_size", [SP, P, i32, i32]),
+                        ("dopd_window_workspace_size", [SP, P, P, i32, i32, i32]),
+                        ("dopd_tree_workspace_size", [SP, P, P, i32])):
             getattr(L, f).argtypes = args
             getattr(L, f).restype = sz
         L.dopd_validate_page_table_host.argtypes = [P, i32, i32, P, i32]
@@ -385,6 +396,87 @@ def dopd_pd_step_fp8(shape, q_dec, dec_page_table, context_lens, context_lens_ho
         "dopd_pd_step_fp8")
 
 
+def dopd_window_workspace_size(shape, cu_seqlens_host, prefix_lens_host, num_reqs, window,
+                               num_sinks=0) -> int:
+    cu_h = _host_i32(cu_seqlens_host)
+    pre_h = _host_i32(prefix_lens_host)
+    return int(lib().dopd_window_workspace_size(C.byref(shape), _hptr(cu_h), _hptr(pre_h),
+                                                int(num_reqs), int(window), int(num_sinks)))
+
+
+def dopd_window_attn(shape, q, k_pool, v_pool, num_pages, page_table, page_table_stride,
+                     cu_seqlens, cu_seqlens_host, prefix_lens, prefix_lens_host, num_reqs, window,
+                     num_sinks, out, lse, workspace, workspace_bytes=None, stream=None):
+    cu_h = _host_i32(cu_seqlens_host)
+    pre_h = _host_i32(prefix_lens_host)
+    _check(_calls().dopd_window_attn(
+        shape, q, k_pool, v_pool, num_pages, page_table, page_table_stride, cu_seqlens, cu_h,
+        prefix_lens, pre_h, num_reqs, window, num_sinks, out, lse, workspace, _nbytes(workspace,
+        workspace_bytes), _stream(stream)),
+        "dopd_window_attn")
+
+
+def dopd_window_attn_fp8(shape, q, k_pool, v_pool, k_scale, v_scale, num_pages, page_table,
+                         page_table_stride, cu_seqlens, cu_seqlens_host, prefix_lens,
+                         prefix_lens_host, num_reqs, window, num_sinks, out, lse, workspace,
+                         workspace_bytes=None, stream=None):
+    cu_h = _host_i32(cu_seqlens_host)
+    pre_h = _host_i32(prefix_lens_host)
+    _check(_calls().dopd_window_attn_fp8(
+        shape, q, k_pool, v_pool, k_scale, v_scale, num_pages, page_table, page_table_stride,
+        cu_seqlens, cu_h, prefix_lens, pre_h, num_reqs, window, num_sinks, out, lse, workspace,
+        _nbytes(workspace, workspace_bytes), _stream(stream)),
+        "dopd_window_attn_fp8")
+
+
+def dopd_tree_workspace_size(shape, cu_seqlens_host, prefix_lens_host, num_reqs) -> int:
+    cu_h = _host_i32(cu_seqlens_host)
+    pre_h = _host_i32(prefix_lens_host)
+    return int(lib().dopd_tree_workspace_size(C.byref(shape), _hptr(cu_h), _hptr(pre_h),
+                                              int(num_reqs)))
+
+
+def dopd_tree_attn(shape, q, k_pool, v_pool, num_pages, page_table, page_table_stride, cu_seqlens,
+                   cu_seqlens_host, prefix_lens, prefix_lens_host, num_reqs, tree_mask, mask_words,
+                   out, lse, workspace, workspace_bytes=None, stream=None):
+    cu_h = _host_i32(cu_seqlens_host)
+    pre_h = _host_i32(prefix_lens_host)
+    _check(_calls().dopd_tree_attn(
+        shape, q, k_pool, v_pool, num_pages, page_table, page_table_stride, cu_seqlens, cu_h,
+        prefix_lens, pre_h, num_reqs, tree_mask, mask_words, out, lse, workspace,
+        _nbytes(workspace, workspace_bytes), _stream(stream)),
+        "dopd_tree_attn")
+
+
+def dopd_tree_attn_fp8(shape, q, k_pool, v_pool, k_scale, v_scale, num_pages, page_table,
+                       page_table_stride, cu_seqlens, cu_seqlens_host, prefix_lens,
+                       prefix_lens_host, num_reqs, tree_mask, mask_words, out, lse, workspace,
+                       workspace_bytes=None, stream=None):
+    cu_h = _host_i32(cu_seqlens_host)
+    pre_h = _host_i32(prefix_lens_host)
+    _check(_calls().dopd_tree_attn_fp8(
+        shape, q, k_pool, v_pool, k_scale, v_scale, num_pages, page_table, page_table_stride,
+        cu_seqlens, cu_h, prefix_lens, pre_h, num_reqs, tree_mask, mask_words, out, lse, workspace,
+        _nbytes(workspace, workspace_bytes), _stream(stream)),
+        "dopd_tree_attn_fp8")
+
+
+def dopd_kv_compact(shape, num_layers, k_pool, v_pool, num_pages, page_table, page_table_stride,
+                    prefix_lens, accepted, num_accepted, max_accepted, num_reqs, stream=None):
+    _check(_calls().dopd_kv_compact(
+        shape, num_layers, k_pool, v_pool, num_pages, page_table, page_table_stride, prefix_lens,
+        accepted, num_accepted, max_accepted, num_reqs, _stream(stream)),
+        "dopd_kv_compact")
+
+
+def dopd_kv_copy_pages(shape, num_layers, k_pool, v_pool, num_pages, src_pages, dst_pages,
+                       num_copies, stream=None):
+    _check(_calls().dopd_kv_copy_pages(
+        shape, num_layers, k_pool, v_pool, num_pages, src_pages, dst_pages, num_copies,
+        _stream(stream)),
+        "dopd_kv_copy_pages")
+
+
 def pd_step_workspace(shape, context_lens_host, num_dec, schedule=DOPD_PD_AUTO, device="cuda"):
     """A 256-byte aligned workspace for dopd_pd_step."""
     import torch
@@ -440,6 +532,30 @@ def prefill_paged_fp8_workspace(shape, cu_seqlens_host, prefix_lens_host, num_re
     ws = torch.empty(n + 256, dtype=torch.uint8, device=device)
     off = (-ws.data_ptr()) % 256
     return ws[off:off + n]
+
+
+def _masked_workspace(n, where, device):
+    import torch
+    if n == 0:
+        raise DopdError(DOPD_ERR_INVALID_SHAPE, where)
+    ws = torch.empty(n + 256, dtype=torch.uint8, device=device)
+    off = (-ws.data_ptr()) % 256
+    return ws[off:off + n]
+
+
+def window_workspace(shape, cu_seqlens_host, prefix_lens_host, num_reqs, window, num_sinks=0,
+                     device="cuda"):
+    """A 256-byte aligned workspace for dopd_window_attn(_fp8)."""
+    return _masked_workspace(
+        dopd_window_workspace_size(shape, cu_seqlens_host, prefix_lens_host, num_reqs, window,
+                                   num_sinks), "dopd_window_workspace_size", device)
+
+
+def tree_workspace(shape, cu_seqlens_host, prefix_lens_host, num_reqs, device="cuda"):
+    """A 256-byte aligned workspace for dopd_tree_attn(_fp8)."""
+    return _masked_workspace(
+        dopd_tree_workspace_size(shape, cu_seqlens_host, prefix_lens_host, num_reqs),
+        "dopd_tree_workspace_size", device)
 
 
 def to_device(a: np.ndarray, device="cuda"):

@@ -8,7 +8,7 @@ import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
-SRC = os.path.join(HERE, "csrc", "dopd_attn.hip")
+SRC = os.path.join(HERE, "csrc", "library.hip")
 LIB = os.path.join(HERE, "libdopd_attn.so")
 MARSHAL_SRC = os.path.join(HERE, "csrc", "marshal.cpp")
 MARSHAL = os.path.join(HERE, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))

@@ -142,7 +142,13 @@ struct Entry<dopd_status(A...)> {
   X(dopd_kv_unpack_from_handoff, "siddddhiddidip")                \
   X(dopd_kv_write_pack_for_handoff, "sddddididhiddp")             \
   X(dopd_pd_step, "sdddhiddddddhidddddiiddidzp")                  \
-  X(dopd_pd_step_fp8, "sdddhiddddddhidddddddiiddidzp")
+  X(dopd_pd_step_fp8, "sdddhiddddddhidddddddiiddidzp")      \
+  X(dopd_window_attn, "sdddididhdhiiidddzp")                      \
+  X(dopd_window_attn_fp8, "sdddddididhdhiiidddzp")                \
+  X(dopd_tree_attn, "sdddididhdhididddzp")                        \
+  X(dopd_tree_attn_fp8, "sdddddididhdhididddzp")                  \
+  X(dopd_kv_copy_pages, "siddiddip")                              \
+  X(dopd_kv_compact, "siddididddiip")
 
 #define WRAP(name, sig)                                                                       \
   Entry<decltype(name)>::Fn f_##name = nullptr;                                               \
