@@ -42,14 +42,12 @@ dopd::MaskRule window_rule(int32_t window, int32_t sinks) {
 }
 dopd::MaskRule tree_rule() { return dopd::MaskRule{1, 0, 0}; }
 
-// Shortest part of an item and what a part costs to begin and to merge, both in
-// tiles of the kernel's keys.
 dopd::MaPlan masked_plan(int which, const dopd_attn_shape* s, const dopd::MaskRule& rule, const int32_t* cu_host,
                          const int32_t* prefix_host, int32_t nreq) {
-  const bool few = which == dopd::kMaFew;
+  const dopd::MaCosts cost = which == dopd::kMaFew ? dopd::MaCosts{s->dtype == DOPD_FP8_E4M3 ? 12 : 8, 16, 4}
+                                                   : dopd::MaCosts{3, 6, 3};
   const int g = s->num_q_heads / s->num_kv_heads;
-  return dopd::ma_plan(rule, dopd::ma_kind(which), cu_host, prefix_host, nreq, g, s->num_kv_heads, machine_shape(),
-                       few ? 8 : 4, few ? 8 : 3);
+  return dopd::ma_plan(rule, dopd::ma_kind(which), cu_host, prefix_host, nreq, g, s->num_kv_heads, machine_shape(), cost);
 }
 
 size_t masked_ws_bytes(const dopd_attn_shape* s, const dopd::MaskRule& rule, const int32_t* cu_host,
@@ -70,15 +68,15 @@ size_t masked_workspace_size(const dopd_attn_shape* s, const dopd::MaskRule& rul
 
 template <int D, bool KV8, bool TREE>
 dopd_status launch_masked(int which, const dopd::MaskedArgs& a, const dopd::MaPlan& p, hipStream_t strm) {
-  const dim3 grid((unsigned)p.blocks), block(256);
+  const dim3 grid = grid_of(p.blocks), block(256);
   if (which == dopd::kMaFew) hipLaunchKernelGGL((dopd::masked_few_kernel<D, KV8, TREE>), grid, block, 0, strm, a);
   else hipLaunchKernelGGL((dopd::masked_rows_kernel<D, KV8, TREE>), grid, block, 0, strm, a);
   const dopd_status st = launch_status();
-  if (st != DOPD_OK || p.slots == 0) return st;
+  if (st != DOPD_OK || p.nwg <= 1) return st;
   if (which == dopd::kMaFew)
-    hipLaunchKernelGGL((dopd::masked_merge_kernel<D, dopd::kMaFew>), dim3((unsigned)p.merges), block, 0, strm, a);
+    hipLaunchKernelGGL((dopd::masked_merge_kernel<D, dopd::kMaFew, TREE>), dim3((unsigned)(p.nwg - 1)), block, 0, strm, a);
   else
-    hipLaunchKernelGGL((dopd::masked_merge_kernel<D, dopd::kMaMany>), dim3((unsigned)(p.merges * 8)), block, 0, strm, a);
+    hipLaunchKernelGGL((dopd::masked_merge_kernel<D, dopd::kMaMany, TREE>), dim3((unsigned)(8 * (p.nwg - 1))), block, 0, strm, a);
   return launch_status();
 }
 
@@ -135,9 +133,8 @@ dopd_status masked_impl(const dopd_attn_shape* s, bool kv8, const void* q, const
   if (s->dtype == DOPD_FP32) {
     const dopd::MaKind kind = dopd::ma_kind(dopd::kMaF32);
     a.scale = s->softmax_scale;
-    a.target = INT32_MAX;
-    const dopd::MaPlan p = dopd::ma_plan_of(rule, kind, cu_host, prefix_host, nreq, hq / hkv, hkv, a.deal, a.target);
-    if (p.blocks > INT32_MAX / 2) return DOPD_ERR_INVALID_SHAPE;
+    const dopd::MaPlan p = dopd::ma_plan(rule, kind, cu_host, prefix_host, nreq, hq / hkv, hkv, machine_shape(), dopd::MaCosts{});
+    if (!p.fits) return DOPD_ERR_INVALID_SHAPE;
     const dim3 grid = grid_of(p.blocks);
     if (d == 64) {
       const dim3 block(64 * dopd::f32_waves<64>());
@@ -156,7 +153,7 @@ dopd_status masked_impl(const dopd_attn_shape* s, bool kv8, const void* q, const
   size_t need = 0;
   for (int which : {dopd::kMaFew, dopd::kMaMany}) {
     plans[which] = masked_plan(which, s, rule, cu_host, prefix_host, nreq);
-    if (plans[which].blocks > (1 << 23) || plans[which].slots > (1 << 23)) return DOPD_ERR_INVALID_SHAPE;
+    if (!plans[which].fits) return DOPD_ERR_INVALID_SHAPE;
     need += dopd::ma_ws_bytes(plans[which], dopd::ma_kind(which), d);
   }
   if (need > 0) {
@@ -169,7 +166,9 @@ dopd_status masked_impl(const dopd_attn_shape* s, bool kv8, const void* q, const
     const dopd::MaPlan& p = plans[which];
     if (p.blocks == 0) continue;
     const dopd::MaKind kind = dopd::ma_kind(which);
-    a.target = p.target;
+    a.nwg = p.nwg;
+    a.seg = p.seg;
+    a.total = (int)p.total;
     a.part_o = reinterpret_cast<float*>(ws);
     a.part_ml = reinterpret_cast<float*>(ws + dopd::ma_part_ml_off(p, kind, d));
     ws += dopd::ma_ws_bytes(p, kind, d);

@@ -30,13 +30,13 @@ struct MaskedArgs {
   const uint32_t* mask;       // [T][words], tree calls only
   void* out;                  // [T][Hq][D]
   float* lse;                 // [T][Hq] or null
-  float* part_o;              // [slots][rows][D]
-  float* part_ml;             // [slots][rows][2]
+  float* part_o;              // [2 nwg][rows][D]
+  float* part_ml;             // [2 nwg][rows][2]
   MaskRule rule;
   MaDeal deal;
   FastDiv by_g;               // (packed rows of a call stay below 2^32 / g: host check)
   int pt_stride, nreq, hq, hkv, words;
-  int target;                 // tiles of a part
+  int nwg, seg, total;        // slices (nwg 0: whole items), see the plan
   float scale;                // softmax scale, times log2(e) but for fp32
 };
 
@@ -78,126 +78,158 @@ __device__ __forceinline__ int seen_page(const MaskedArgs& a, int t, int low_key
   return t * kPage >= a.rule.sinks && t < low ? low : min(t, (end - 1) / kPage);
 }
 
-// A workgroup's part of a call.
+// A workgroup's item, or the part of one that lies in its slice.
 struct MaItem {
-  int req, c, rt, split, nsplit;
+  int req, c, rt;
   int row0, n, pre;  // the request's rows of q, its tokens, its cached tokens
-  int64_t slot;      // of its partial result
+  int u0, u1;        // units of the item's span [u0, u1) in the slice (whole items: all)
+  int slot;          // of a partial result
 };
 
-// Part of workgroup b (the same in every lane of every wave); false: none.
-template <int KIND>
-__device__ __forceinline__ bool ma_find(const MaskedArgs& a, int b, MaItem& it) {
+// The request that unit (or block) x of the call lies in, and x's offset in it;
+// count(r, n, pre): the units of request r.  The same in every lane; every wave takes
+// part.  false: past the last one.
+template <int KIND, class Count>
+__device__ __forceinline__ bool ma_find(const MaskedArgs& a, int x, Count count, MaItem& it, int& local) {
   constexpr MaKind kind = ma_kind(KIND);
-  constexpr int ROWS = kind.rows;
   const int l = lane_id(), g = (int)a.by_g.d;
   int base = 0;
-  int64_t slots = 0;
   for (int r0 = 0; r0 < a.nreq; r0 += 64) {
     const int r = min(r0 + l, a.nreq - 1);
     const int row0 = a.cu[r], n = a.cu[r + 1] - row0, pre = a.prefix[r];
-    int blocks = 0, s = 1, rt = 0;
-    if (r0 + l < a.nreq && ma_mine(kind, n, g)) {
-      rt = ma_row_tiles(n, g, ROWS);
-      s = ma_splits(ma_most_tiles(a.rule, pre, n, g, kind), a.target);
-      blocks = (int)ma_blocks(a.deal, a.hkv, (int64_t)rt * s);
-    }
-    const int sl = s > 1 ? a.hkv * rt * s : 0;
-    const int incl = wave_inclusive_scan(blocks), incl_s = wave_inclusive_scan(sl);
+    const int mine = r0 + l < a.nreq && ma_mine(kind, n, g) ? count(n, pre) : 0;
+    const int incl = wave_inclusive_scan(mine);
     const int total = __builtin_amdgcn_readlane(incl, 63);
-    if (b < base + total) {
-      const int o = __ffsll((long long)__ballot(b - base < incl)) - 1;
-      auto of = [&](int v) { return __builtin_amdgcn_readlane(v, o); };
-      const int local = b - base - of(incl - blocks);
-      const int parts = of(rt) * of(s);
+    if (x < base + total) {
+      const int o = __ffsll((long long)__ballot(x - base < incl)) - 1;
+      local = x - base - __builtin_amdgcn_readlane(incl - mine, o);
       it.req = r0 + o;
-      it.nsplit = of(s);
-      it.row0 = of(row0);
-      it.n = of(n);
-      it.pre = of(pre);
-      int idx;
-      if (!ma_part(a.deal, a.hkv, parts, local, it.c, idx)) return false;
-      it.split = idx / of(rt);
-      it.rt = idx - it.split * of(rt);
-      it.slot = slots + of(incl_s - sl) + (int64_t)it.c * parts + idx;
+      it.row0 = __builtin_amdgcn_readlane(row0, o);
+      it.n = __builtin_amdgcn_readlane(n, o);
+      it.pre = __builtin_amdgcn_readlane(pre, o);
       return true;
     }
     base += total;
-    slots += __builtin_amdgcn_readlane(incl_s, 63);
   }
   return false;
 }
 
-// The merge of the split items: workgroup = 16 packed rows of one item, thread = a
-// 4-dim chunk of a row, the item's partials folded in key order:
+// Calls body(item) for each item of workgroup b (uniform).
+template <int KIND, class Body>
+__device__ __forceinline__ void ma_items(const MaskedArgs& a, int b, Body body) {
+  constexpr MaKind kind = ma_kind(KIND);
+  const int g = (int)a.by_g.d;
+  MaItem it;
+  int local, begin = 0, pos = 0, end = 0, slice = 0;
+  auto units = [&](int n, int pre) {
+    return a.hkv * ma_row_tiles(n, g, kind.rows) * (int)ma_span_units(a.rule, pre, n, g, kind, a.seg);
+  };
+  if (a.nwg == 0) {
+    auto blocks = [&](int n, int) { return (int)ma_blocks(a.deal, a.hkv, ma_row_tiles(n, g, kind.rows)); };
+    if (!ma_find<KIND>(a, b, blocks, it, local)) return;
+    if (!ma_part(a.deal, a.hkv, ma_row_tiles(it.n, g, kind.rows), local, it.c, it.rt)) return;
+  } else {
+    slice = ma_slice_index(b, a.nwg, a.deal.xcds);
+    begin = pos = (int)ma_slice_begin(slice, a.total, a.nwg);
+    end = (int)ma_slice_begin(slice + 1, a.total, a.nwg);
+    if (pos >= end || !ma_find<KIND>(a, pos, units, it, local)) return;
+  }
+  while (true) {  // slices: one item, or part of one, at a time
+    if (a.nwg != 0) {
+      const int span = (int)ma_span_units(a.rule, it.pre, it.n, g, kind, a.seg), rts = ma_row_tiles(it.n, g, kind.rows);
+      const int index = local / span;
+      it.u0 = local - index * span;
+      it.u1 = min(span, it.u0 + end - pos);
+      it.c = index / rts;
+      it.rt = index - it.c * rts;
+      it.slot = 2 * slice + (pos == begin ? 0 : 1);
+      pos += it.u1 - it.u0;
+      local += it.u1 - it.u0;
+    }
+    if (a.nwg == 0 || it.u1 > a.seg) body(it);  // (else only units of the start)
+    if (pos >= end) return;
+    if (local == units(it.n, it.pre)) {  // the next request of this kernel
+      do {
+        ++it.req;
+        it.row0 = __builtin_amdgcn_readfirstlane(a.cu[it.req]);
+        it.n = __builtin_amdgcn_readfirstlane(a.cu[it.req + 1]) - it.row0;
+      } while (!ma_mine(kind, it.n, g));
+      it.pre = __builtin_amdgcn_readfirstlane(a.prefix[it.req]);
+      local = 0;
+    }
+  }
+}
+
+// Tiles [v0, v1) of an item of n tiles that its units cover, and whether that is all
+// of it.  (A span can be longer than the item: ma_most_tiles is a bound.)
+__device__ __forceinline__ bool ma_tiles_of(const MaskedArgs& a, const MaItem& it, int n, int& v0, int& v1) {
+  v0 = a.nwg == 0 ? 0 : min(n, max(0, it.u0 - a.seg));
+  v1 = a.nwg == 0 ? n : min(n, it.u1 - a.seg);
+  return v0 == 0 && v1 == n;
+}
+
+// The merge of the items that lie in several slices: workgroup = 16 packed rows of
+// the item that slice 1 + blockIdx.x / (rows / 16) continues, if that slice is the
+// first to continue it; thread = a 4-dim chunk of a row, the partials folded in key
+// order:
 //   M = max_s m_s,  L = sum_s 2^(m_s - M) l_s,  o = sum_s 2^(m_s - M) o~_s / L.
-// Bound by the partials' bytes (HBM or the caches); several workgroups an item,
-// since one alone reads 16 partials of 64 KiB in about 15 us.
-template <int D, int KIND>
+// Bound by the partials' bytes and the start of a kernel.
+template <int D, int KIND, bool TREE>
 __global__ __launch_bounds__(256) void masked_merge_kernel(MaskedArgs a) {
   constexpr MaKind kind = ma_kind(KIND);
-  constexpr int ROWS = kind.rows;
-  constexpr int kGroup = 16;
-  const int l = lane_id(), g = (int)a.by_g.d;
-  const int item = (int)blockIdx.x / (ROWS / kGroup), part = (int)blockIdx.x % (ROWS / kGroup);
-  int rt_l = 0, s_l = 1, row0_l = 0, n_l = 0, slots_l = 0;
-  int64_t slots = 0;
-  int base = 0, r = -1, local = 0;
-  for (int r0 = 0; r0 < a.nreq; r0 += 64) {
-    const int rr = min(r0 + l, a.nreq - 1);
-    row0_l = a.cu[rr];
-    n_l = a.cu[rr + 1] - row0_l;
-    rt_l = 0;
-    s_l = 1;
-    if (r0 + l < a.nreq && ma_mine(kind, n_l, g)) {
-      rt_l = ma_row_tiles(n_l, g, ROWS);
-      s_l = ma_splits(ma_most_tiles(a.rule, a.prefix[rr], n_l, g, kind), a.target);
-    }
-    const int items = s_l > 1 ? a.hkv * rt_l : 0;
-    slots_l = items * s_l;
-    const int incl = wave_inclusive_scan(items), incl_s = wave_inclusive_scan(slots_l);
-    const int total = __builtin_amdgcn_readlane(incl, 63);
-    if (item < base + total) {
-      const int o = __ffsll((long long)__ballot(item - base < incl)) - 1;
-      r = o;
-      local = item - base - __builtin_amdgcn_readlane(incl - items, o);
-      slots += __builtin_amdgcn_readlane(incl_s - slots_l, o);
-      break;
-    }
-    base += total;
-    slots += __builtin_amdgcn_readlane(incl_s, 63);
-  }
-  if (r < 0) return;
-  const int rt = __builtin_amdgcn_readlane(rt_l, r), s = __builtin_amdgcn_readlane(s_l, r);
-  const int row0 = __builtin_amdgcn_readlane(row0_l, r), n = __builtin_amdgcn_readlane(n_l, r);
-  const int c = local / rt, tile = local - c * rt;
-  const int64_t slot0 = slots + (int64_t)c * rt * s + tile;  // of split u: slot0 + u * rt
-  const int live = min(ROWS, n * g - tile * ROWS);
-  constexpr int CH = D / 4;
+  constexpr int ROWS = kind.rows, kGroup = 16, CH = D / 4;
+  const int g = (int)a.by_g.d;
+  const int slice = 1 + (int)blockIdx.x / (ROWS / kGroup), group = (int)blockIdx.x % (ROWS / kGroup);
+  MaItem it;
+  int local;
+  const int at = (int)ma_slice_begin(slice, a.total, a.nwg);
+  auto units = [&](int n, int pre) {
+    return a.hkv * ma_row_tiles(n, g, ROWS) * (int)ma_span_units(a.rule, pre, n, g, kind, a.seg);
+  };
+  if (at >= a.total || !ma_find<KIND>(a, at, units, it, local)) return;
+  const int span = (int)ma_span_units(a.rule, it.pre, it.n, g, kind, a.seg), rts = ma_row_tiles(it.n, g, ROWS);
+  const int index = local / span, c = index / rts, rt = index - c * rts;
+  const int x0 = rt * ROWS, live = min(ROWS, it.n * g - x0);
+  if (group * kGroup >= live) return;
+  const int p0 = it.pre + fast_quot(x0, a.by_g), p1 = it.pre + fast_quot(x0 + live - 1, a.by_g);
+  const int tiles = ma_key_tiles(a.rule, p0, TREE ? it.pre + it.n - 1 : p1, kind.keys).n;
+  const int first = at - (local - index * span);  // the item's first unit
+  const int b0 = (int)ma_slice_of(first + a.seg, a.total, a.nwg);
+  const int b1 = (int)ma_slice_of(first + a.seg + tiles - 1, a.total, a.nwg);
+  if (b0 == b1 || slice != b0 + 1) return;
+  const int slot0 = 2 * b0 + (ma_slice_begin(b0, a.total, a.nwg) >= first ? 0 : 1);
   for (int i = (int)threadIdx.x; i < kGroup * CH; i += 256) {
-    const int row = kGroup * part + i / CH, e0 = 4 * (i % CH);
+    const int row = kGroup * group + i / CH, e0 = 4 * (i % CH);
     if (row >= live) break;
-    float M = -INFINITY;
-    for (int u = 0; u < s; ++u) M = fmaxf(M, a.part_ml[((slot0 + (int64_t)u * rt) * ROWS + row) * 2]);
-    float L = 0.f;
+    float M = -INFINITY, L = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int u = 0; u < s; ++u) {
-      const int64_t at = (slot0 + (int64_t)u * rt) * ROWS + row;
-      const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + at * 2);
-      const f32x4 o = *reinterpret_cast<const f32x4*>(a.part_o + at * D + e0);
-      const float w = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);  // (a part that saw nothing)
-      L += w * ml.y;
-      acc += o * w;
+    for (int b = b0; b <= b1; b += 4) {  // four partials in flight
+      float2 ml[4];
+      f32x4 o[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int64_t from = (int64_t)(b + u == b0 ? slot0 : 2 * min(b + u, b1)) * ROWS + row;
+        ml[u] = *reinterpret_cast<const float2*>(a.part_ml + from * 2);
+        o[u] = *reinterpret_cast<const f32x4*>(a.part_o + from * D + e0);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (b + u > b1 || ml[u].x == -INFINITY) continue;  // (a part that saw nothing of the row)
+        const float m = fmaxf(M, ml[u].x);
+        const float old = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - m), now = __builtin_amdgcn_exp2f(ml[u].x - m);
+        L = L * old + ml[u].y * now;
+        acc = acc * old + o[u] * now;
+        M = m;
+      }
     }
     const float inv = L == 0.f ? 0.f : 1.f / L;
-    const int x = tile * ROWS + row, tok = fast_quot(x, a.by_g);
-    const int64_t at = (int64_t)(row0 + tok) * a.hq + c * g + (x - tok * g);
-    u32x2 w2;
-    w2[0] = pack_bf16x2(acc[0] * inv, acc[1] * inv);
-    w2[1] = pack_bf16x2(acc[2] * inv, acc[3] * inv);
-    *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + at * D + e0) = w2;
-    if (a.lse && e0 == 0) a.lse[at] = (M + __log2f(L)) * kLn2;
+    const int x = x0 + row, tok = fast_quot(x, a.by_g);
+    const int64_t to = (int64_t)(it.row0 + tok) * a.hq + c * g + (x - tok * g);
+    u32x2 w;
+    w[0] = pack_bf16x2(acc[0] * inv, acc[1] * inv);
+    w[1] = pack_bf16x2(acc[2] * inv, acc[3] * inv);
+    *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + to * D + e0) = w;
+    if (a.lse && e0 == 0) a.lse[to] = (M + __log2f(L)) * kLn2;
   }
 }
 

@@ -24,8 +24,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void masked_f32_kernel(MaskedArgs a)
   __shared__ float s_o[W][ROWS][OP];
   __shared__ float s_m[W][ROWS], s_l[W][ROWS];
 
-  MaItem it;
-  if (!ma_find<kMaF32>(a, grid_block(blockIdx.x, blockIdx.y), it)) return;  // uniform
+  ma_items<kMaF32>(a, grid_block(blockIdx.x, blockIdx.y), [&](const MaItem& it) {
   const int l = lane_id(), w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int g = (int)a.by_g.d, c = it.c, hkv = a.hkv;
   const int rows = it.n * g, x0 = it.rt * ROWS, last_row = min(rows, x0 + ROWS) - 1;
@@ -165,6 +164,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void masked_f32_kernel(MaskedArgs a)
     static_cast<float*>(a.out)[at * D + e] = sum == 0.f ? 0.f : F32Quot(sum)(acc);
     if (a.lse && e == 0) a.lse[at] = M + logf(sum);
   }
+  });
 }
 
 }  // namespace dopd

@@ -1,8 +1,9 @@
 // Windowed and tree attention for requests of at most 16 packed rows (decode
 // steps, small trees), bf16 in / fp32 accumulate, over bf16 or E4M3 pages.
 //
-// Workgroup = 4 waves = one part of one (request, KV head): up to a.target visited
-// pairs of pages (32 keys), taken by the waves in turn and merged through LDS.
+// Workgroup = 4 waves = one (request, KV head), or a slice of the call's items: the
+// visited pairs of pages (32 keys) are taken by the waves in turn and merged through
+// LDS.
 // Per pair and wave, the packed rows being the 16 MFMA columns,
 //   S^T[32 keys][16] = K[32][d] . Q^T[d][16]     2 x (d / 32) v_mfma_f32_16x16x32_bf16
 //   O^T[d][16]      += V^T[d][32] . P^T[32][16]  (d / 16) of them
@@ -80,14 +81,15 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void masked_few_kernel(MaskedArg
   __shared__ __attribute__((aligned(16))) f32x4 s_o[W][NT * 64];
   __shared__ float s_m[W][16], s_l[W][16];
 
-  MaItem it;
-  if (!ma_find<kMaFew>(a, (int)blockIdx.x, it)) return;  // uniform
+  ma_items<kMaFew>(a, grid_block(blockIdx.x, blockIdx.y), [&](const MaItem& it) {
   const int l = lane_id(), w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int g = (int)a.by_g.d, c = it.c, hkv = a.hkv;
   const int rows = it.n * g;
   const int pre = it.pre, end = pre + it.n, p1 = end - 1;
   const KeyTiles kt = ma_key_tiles(a.rule, pre, p1, KEYS);
-  const int v0 = (int)((int64_t)it.split * kt.n / it.nsplit), v1 = (int)((int64_t)(it.split + 1) * kt.n / it.nsplit);
+  int v0, v1;
+  const bool whole = ma_tiles_of(a, it, kt.n, v0, v1);
+  if (v0 >= v1) return;
   const int low_key = ma_low_key(a.rule, pre);
 
   const int col = l & 15, qg = l >> 4;  // MFMA column = packed row; lane group = k-slot group
@@ -245,7 +247,6 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void masked_few_kernel(MaskedArg
     L += f[u] * s_l[u][col];
   }
   const float vsc = KV8 ? a.v_scale[c] : 1.f;
-  const bool whole = it.nsplit == 1;
   const float fac = !whole ? vsc : L == 0.f ? 0.f : vsc / L;
 #pragma unroll
   for (int n0 = 0; n0 < NT; n0 += W) {
@@ -261,13 +262,15 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void masked_few_kernel(MaskedArg
       o2[1] = pack_bf16x2(o[2], o[3]);
       *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + qrow * D + 16 * n + 4 * qg) = o2;
     } else {
-      *reinterpret_cast<f32x4*>(a.part_o + (it.slot * ROWS + col) * D + 16 * n + 4 * qg) = o;
+      *reinterpret_cast<f32x4*>(a.part_o + ((int64_t)it.slot * ROWS + col) * D + 16 * n + 4 * qg) = o;
     }
   }
   if (w == 0 && qg == 0 && col < rows) {
-    if (!whole) *reinterpret_cast<float2*>(a.part_ml + (it.slot * ROWS + col) * 2) = float2{M, L};
+    if (!whole) *reinterpret_cast<float2*>(a.part_ml + ((int64_t)it.slot * ROWS + col) * 2) = float2{M, L};
     else if (a.lse) a.lse[qrow] = (M + __log2f(L)) * kLn2;
   }
+  __syncthreads();  // the next item reuses the merge buffers
+  });
 }
 
 }  // namespace dopd

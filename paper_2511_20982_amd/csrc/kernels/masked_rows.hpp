@@ -1,8 +1,8 @@
 // Windowed and tree attention for requests of more than 16 packed rows (chunks,
 // larger trees), bf16 in / fp32 accumulate, over bf16 or E4M3 pages.
 //
-// Workgroup = 4 waves = one part of an item of 128 packed rows of one (request, KV
-// head), 32 rows a wave; two workgroups share a CU.  Packing the g query heads of a
+// Workgroup = 4 waves = an item of 128 packed rows of one (request, KV head), 32 rows
+// a wave, or a slice of the call's items; two workgroups share a CU.  Packing the g query heads of a
 // KV head into the rows lets 128 / g tokens share a tile, so that a window's
 // ragged ends take few masked tiles and a small tree fills the matrix units.  Per
 // visited tile of 64 keys and wave
@@ -29,11 +29,13 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
   constexpr int NCH8 = D / 16;  // E4M3: 16-byte chunks of a K row
   constexpr int TE = rows_tile_elems<D, KV8>();
   constexpr int RS = D + 8;     // padded row of the output staging
-  constexpr int kStage = 32 * RS > TE ? 32 * RS : TE;  // (a wave's output block reuses a tile buffer)
+  constexpr int kStage = 32 * RS + 8 > TE ? 32 * RS + 8 : TE;  // (a wave's output block reuses a tile buffer)
   __shared__ __attribute__((aligned(16))) uint16_t sK0[kStage], sK1[kStage], sV0[kStage], sV1[kStage];
+  // Q operands KS / 2 .. of every lane, which masked steps read from here: held in
+  // registers there too, some were spilled, and a reload waits for the tiles in flight.
+  __shared__ __attribute__((aligned(16))) uint16_t sQ[KS / 2 * kRowsThreads * 8];
 
-  MaItem it;
-  if (!ma_find<kMaMany>(a, (int)blockIdx.x, it)) return;  // uniform
+  ma_items<kMaMany>(a, grid_block(blockIdx.x, blockIdx.y), [&](const MaItem& it) {
   const int tid = (int)threadIdx.x, l = lane_id();
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = (int)a.by_g.d, c = it.c, hkv = a.hkv;
@@ -44,7 +46,9 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
   const int p0 = pre + fast_quot(x0, a.by_g), p1 = pre + fast_quot(last_row, a.by_g);
   const int end = TREE ? pre + it.n : p1 + 1;  // keys of the item: below this
   const KeyTiles kt = ma_key_tiles(a.rule, p0, end - 1, KEYS);
-  const int v0 = (int)((int64_t)it.split * kt.n / it.nsplit), v1 = (int)((int64_t)(it.split + 1) * kt.n / it.nsplit);
+  int v0, v1;
+  const bool whole = ma_tiles_of(a, it, kt.n, v0, v1);
+  if (v0 >= v1) return;
   const int low_key = ma_low_key(a.rule, p0);
 
   const int hi = l >> 5;
@@ -56,15 +60,20 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
   const uint32_t* mrow = TREE ? a.mask + (int64_t)(it.row0 + tok) * a.words : nullptr;
 
   // Q^T operand: Q[row][16 ks + 8 hi + 0..7] (E4M3: the dims a 16-byte read of a K
-  // row gives a lane over two k-steps).
-  bf16x8 qop[KS];
+  // row gives a lane over two k-steps).  The upper half stays in LDS (this lane's own
+  // slots: no barrier needed) and comes to registers for runs of full tiles.
+  constexpr int KH = KS / 2;
+  bf16x8 qlo[KH];
   {
     const uint16_t* qp = static_cast<const uint16_t*>(a.q) + qrow * D + (KV8 ? 16 : 8) * hi;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
-      qop[ks] = __builtin_bit_cast(
-          bf16x8, *reinterpret_cast<const u32x4*>(qp + (KV8 ? 32 * (ks / 2) + 8 * (ks % 2) : 16 * ks)));
+    for (int ks = 0; ks < KS; ++ks) {
+      const u32x4 q = *reinterpret_cast<const u32x4*>(qp + (KV8 ? 32 * (ks / 2) + 8 * (ks % 2) : 16 * ks));
+      if (ks < KH) qlo[ks] = __builtin_bit_cast(bf16x8, q);
+      else *reinterpret_cast<u32x4*>(sQ + ((ks - KH) * kRowsThreads + tid) * 8) = q;
+    }
   }
+  auto qhi_lds = [&](int i) { return *reinterpret_cast<const bf16x8*>(sQ + (i * kRowsThreads + tid) * 8); };
   f32x16 oacc[ET];
 #pragma unroll
   for (int et = 0; et < ET; ++et)
@@ -72,8 +81,6 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
     for (int i = 0; i < 16; ++i) oacc[et][i] = 0.f;
   float m_run = -INFINITY, l_run = 0.f;
   const float c_in = KV8 ? a.scale * a.k_scale[c] : a.scale;
-  const bool pos = c_in > 0.f;  // else scores are scaled before their maximum is taken
-  const float c_eff = pos ? c_in : 1.f;
 
   // ---- tiles: wave w brings page w of a tile.  K (bf16) in 16-byte chunks,
   // [D / 32 chunk groups][64 rows][4 slots], chunk ch of row t in slot (ch % 4) ^
@@ -104,10 +111,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
           16, lane_off, step * u, 0, 0);
   };
   // (E4M3 K: rows s and s + 8 of a page block are page slots pi(s) and pi(s) + 4.)
-  auto load_tile = [&](uint16_t* k, uint16_t* v, int page) {
-    stage(a.k_pool, k, page, lane_k, KV8 ? 4 * D : 64);
-    stage(a.v_pool, v, page, lane_v, KV8 ? 1024 : 64 * kPage);
-  };
+  constexpr int kStepK = KV8 ? 4 * D : 64, kStepV = KV8 ? 1024 : 64 * kPage;
 
   // A operands of the QK MFMA: K[32 tt + l % 32][16 ks + 8 hi + 0..7].
   const int kr_m = hi ^ ((l >> 2) & 3);
@@ -138,133 +142,276 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
   };
 
   bf16x8 p[4];  // P^T: B operands of the four P.V k-steps
-  // Weights against m_use; returns this lane's half of the row sum.
-  auto weights = [&](const f32x16 (&s)[2], float m_use) {
+  // Weights 2^(c s - m_use); returns this lane's half of the row sum.
+  auto weights = [&](const f32x16 (&s)[2], float c, float m_use) {
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[tt][i], c_eff, -m_use));
+        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[tt][i], c, -m_use));
         sum[i & 3] += e;
         p[2 * tt + (i >> 3)][i & 7] = (__bf16)e;
       }
     return (sum[0] + sum[1]) + (sum[2] + sum[3]);
   };
-  auto raise_max = [&](const f32x16 (&s)[2]) {
+  auto row_max = [&](const f32x16 (&s)[2]) {
     float mx = __builtin_elementwise_maximum(s[0][0], s[1][0]);
 #pragma unroll
     for (int i = 1; i < 16; ++i) mx = __builtin_elementwise_maximum(mx, __builtin_elementwise_maximum(s[0][i], s[1][i]));
     const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-    mx = __builtin_elementwise_maximum(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * c_eff;
-    // The running maximum moves only where a tile raises it by more than 8 (log2), so
-    // that most tiles rescale nothing; the weights then stay below 2^8.
-    if (__ballot(!(mx <= m_run + 8.f)) == 0) return;  // (a NaN moves it too; -inf: stays)
-    const float m_new = fmaxf(m_run, mx);
+    return __builtin_elementwise_maximum(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+  };
+  // The running maximum becomes m_new; O and the row sum follow.
+  auto rescale = [&](float m_new) {
     const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
     m_run = m_new;
     l_run *= alpha;
 #pragma unroll
     for (int et = 0; et < ET; ++et) oacc[et] *= alpha;
   };
-
-  auto step = [&](const uint16_t* sk, const uint16_t* sv, int v) {
-    const int base = KEYS * ma_tile(kt, v);
-    f32x16 s[2];
+  // S^T of a tile; qhi(i): Q operand KH + i.
+  auto qk = [&](const uint16_t* sk, f32x16 (&s)[2], auto qhi) {
+    bf16x8 ka[2][KS];
+    kread(sk, 0, ka[0]);
+    kread(sk, 1, ka[1]);
 #pragma unroll
-    for (int tt = 0; tt < 2; ++tt) {
+    for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[tt][i] = 0.f;
-      bf16x8 ka[KS];
-      kread(sk, tt, ka);
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) s[tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[ks], qop[ks], s[tt], 0, 0, 0);
+    for (int ks = 0; ks < KS; ++ks) {
+      const bf16x8 qv = ks < KH ? qlo[ks < KH ? ks : 0] : qhi(ks - KH);
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) s[tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[tt][ks], qv, s[tt], 0, 0, 0);
     }
-    const bool full = all_see<TREE>(a, base, KEYS, pre, p0, p1);  // uniform
-    if (full && pos) {
-      // No maximum is taken: the weights are formed against the running one, and only
-      // a sum beyond 2^20 (a tile far above it; the first one seen) takes it.
-      float sum = weights(s, m_run);
-      if (__ballot(!(sum <= 1048576.f))) {
-        raise_max(s);
-        sum = weights(s, m_run);
-      }
-      l_run += sum;
+  };
+  auto pv = [&](const uint16_t* sv) {
 #pragma unroll
-      for (int kk = 0; kk < 4; ++kk)
+    for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
-        for (int et = 0; et < ET; ++et)
-          oacc[et] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vread(sv, kk, et)), p[kk],
-                                                             oacc[et], 0, 0, 0);
-      return;
-    }
-    uint32_t sees[2], live[2];
+      for (int et = 0; et < ET; ++et)
+        oacc[et] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vread(sv, kk, et)), p[kk], oacc[et], 0,
+                                                           0, 0);
+  };
+  // Scales the scores and makes those of what a row does not see -inf; sees: by 32
+  // keys of the tile.  (Scaled here, not in the exponent, for scales of any sign.)
+  auto hide = [&](f32x16 (&s)[2], int base, uint32_t (&sees)[2]) {
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
-      if (!pos) s[tt] *= c_in;
-      sees[tt] = row_sees<TREE>(a, base + 32 * tt, pre, end, pre + tok, mrow);
-      live[tt] = any_sees<TREE>(a, base + 32 * tt, p0, end) >> (8 * hi);
+      sees[tt] = row_sees<TREE>(a, base + 32 * tt, pre, end, pre + tok, mrow) >> (8 * hi);
 #pragma unroll
       for (int i = 0; i < 16; ++i)  // accumulator row i is key 16 (i / 8) + 8 hi + i % 8
-        if (!(sees[tt] >> (16 * (i >> 3) + 8 * hi + (i & 7)) & 1)) s[tt][i] = -INFINITY;
+        s[tt][i] = sees[tt] >> (16 * (i >> 3) + (i & 7)) & 1 ? s[tt][i] * c_in : -INFINITY;
     }
-    raise_max(s);
-    l_run += weights(s, m_run == -INFINITY ? 0.f : m_run);  // (nothing seen so far: weights 0)
+  };
+  // V of positions of visited tile v that no row of the item sees (slots that may hold
+  // anything: 0 * NaN is NaN) is cleared in LDS by the wave that brought its page, once
+  // that has landed; the barrier that ends the step publishes it.
+  auto clear_dead = [&](uint16_t* sv, int v) {
+    if (v >= v1) return;
+    const uint32_t live = any_sees<TREE>(a, KEYS * ma_tile(kt, v) + kPage * w, p0, end) & 0xffff;  // uniform
+    if (live == 0xffff) return;
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
+    if constexpr (KV8) {  // [D dim rows][16 key bytes]
+      u32x4 keep;
 #pragma unroll
-    for (int kk = 0; kk < 4; ++kk) {
-      const uint32_t keep = live[kk >> 1] >> (16 * (kk & 1));
-      u32x4 va[ET];
-      u16x2 top = {0, 0};
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t b = live >> (4 * i);
+        keep[i] = (b & 1 ? 0xffu : 0u) | (b & 2 ? 0xff00u : 0u) | (b & 4 ? 0xff0000u : 0u) | (b & 8 ? 0xff000000u : 0u);
+      }
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) {
+        u32x4* x = reinterpret_cast<u32x4*>(reinterpret_cast<uint8_t*>(sv) + w * (kPage * D) + (l + 64 * i) * 16);
+        *x &= keep;
+      }
+    } else {
 #pragma unroll
       for (int et = 0; et < ET; ++et) {
-        va[et] = keep_bf16x8(vread(sv, kk, et), keep);
-        top = max_magnitude(va[et], top);
-      }
-      if (!any_non_finite(top)) {
-#pragma unroll
-        for (int et = 0; et < ET; ++et)
-          oacc[et] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, va[et]), p[kk], oacc[et], 0, 0, 0);
-      } else {
-        for (int r = 0; r < 32; ++r) {  // row r alone, V cleared where it sees nothing
-          const uint32_t see = (uint32_t)__builtin_amdgcn_readlane((int)sees[kk >> 1], r) >> (16 * (kk & 1) + 8 * hi);
-#pragma unroll
-          for (int et = 0; et < ET; ++et) {
-            const f32x16 o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                __builtin_bit_cast(bf16x8, keep_bf16x8(va[et], see)), p[kk], oacc[et], 0, 0, 0);
-            if ((l & 31) == r) oacc[et] = o;
-          }
-        }
+        u32x4* x = reinterpret_cast<u32x4*>(sv + ((et * 8 + 2 * w + hi) * 32 + (l & 31)) * 8);
+        *x = keep_bf16x8(*x, live >> (8 * hi));
       }
     }
   };
+  // Do all rows of the item see all of visited tile v? (uniform)
+  auto full = [&](int v) { return c_in > 0.f && all_see<TREE>(a, KEYS * ma_tile(kt, v), KEYS, pre, p0, p1); };
+  // End of the run of full tiles that v begins.
+  auto run_end = [&](int v) {
+    if constexpr (TREE) return min(v1, pre / KEYS);
+    const int base = KEYS * ma_tile(kt, v);
+    return min(v1, base > p1 - a.rule.window ? (p0 + 1) / KEYS - kt.low + kt.nsink : min(p0 + 1, a.rule.sinks) / KEYS);
+  };
 
-  // Tile v sits in buffer (v - v0) % 2.  One barrier a step: it waits for the tile's
-  // loads and for the waves that still read the buffer the next loads go into.
-  if (v0 < v1) {
-    load_tile(sK0, sV0, __builtin_amdgcn_readfirstlane(page_of(v0)));
-    int ahead = page_of(v0 + 1);
-    int v = v0;
-    while (true) {
+  // K tile i (of v0 + i) sits in K buffer i % 2, V tile i in V buffer i % 2, K a tile
+  // ahead.  Step i loads K tile i + 2 and V tile i + 1 and, after (or while) it forms
+  // the weights of tile i, computes S^T of tile i + 1; the barrier that ends it waits
+  // for the loads and for the waves that read what the next ones replace.
+  int pid_k, pid_v, ahead;
+  auto kbuf = [&](int b) { return b ? sK1 : sK0; };
+  auto vbuf = [&](int b) { return b ? sV1 : sV0; };
+  auto prefetch = [&](int par, int v) {
+    if (v + 2 < v1) stage(a.k_pool, kbuf(par), pid_k, lane_k, kStepK);
+    if (v + 1 < v1) stage(a.v_pool, vbuf(par ^ 1), pid_v, lane_v, kStepV);
+    pid_v = pid_k;
+    pid_k = __builtin_amdgcn_readfirstlane(ahead);  // (landed at the last barrier)
+    ahead = page_of(v + 4);
+  };
+  {
+    const int first = __builtin_amdgcn_readfirstlane(page_of(v0));
+    pid_v = __builtin_amdgcn_readfirstlane(page_of(v0 + 1));
+    stage(a.k_pool, sK0, first, lane_k, kStepK);
+    if (v0 + 1 < v1) stage(a.k_pool, sK1, pid_v, lane_k, kStepK);
+    stage(a.v_pool, sV0, first, lane_v, kStepV);
+    pid_k = __builtin_amdgcn_readfirstlane(page_of(v0 + 2));
+    ahead = page_of(v0 + 3);
+    clear_dead(sV0, v0);
+  }
+  __syncthreads();
+  f32x16 sa[2], sb[2];  // S^T of two consecutive tiles
+  if (active) {
+    qk(sK0, sa, qhi_lds);
+    if (full(v0)) m_run = row_max(sa) * c_in;
+  }
+  __syncthreads();  // (K tile 2 goes where tile 0 was)
+
+  int v = v0;
+  auto even = [] { return 0; };
+  auto odd = [] { return 1; };
+  // A tile that some row does not see in full.
+  auto step_masked = [&](auto par) {
+    prefetch(par(), v);
+    uint32_t sees[2];
+    hide(sa, KEYS * ma_tile(kt, v), sees);
+    rescale(fmaxf(m_run, row_max(sa)));
+    l_run += weights(sa, 1.f, m_run == -INFINITY ? 0.f : m_run);  // (nothing seen so far: weights 0)
+    pv(vbuf(par()));
+    qk(kbuf(par() ^ 1), sa, qhi_lds);
+    clear_dead(vbuf(par() ^ 1), v + 1);
+    __syncthreads();
+    ++v;
+  };
+  // A full tile.  No maximum is taken: the weights are formed against the running
+  // one, and only a sum beyond 2^20 (a tile far above it, the first one seen) takes it.
+  bf16x8 qhi[KH];
+  auto qhi_reg = [&](int i) { return qhi[i]; };
+  auto step_full = [&](f32x16 (&sc)[2], f32x16 (&sn)[2], auto par) {
+    prefetch(par(), v);
+    qk(kbuf(par() ^ 1), sn, qhi_reg);
+    if constexpr (!KV8) {
+      // The K reads spread over the products: all of them ahead, Q operands are
+      // spilled, and a reload waits for the tiles in flight.
+      constexpr int kMfma = 0x008, kDsRead = 0x100, kAhead = KS + 2;
+      __builtin_amdgcn_sched_group_barrier(kDsRead, kAhead, 0);
+#pragma unroll
+      for (int i = 0; i < (2 * KS - kAhead + 1) / 2; ++i) {
+        __builtin_amdgcn_sched_group_barrier(kMfma, 2, 0);
+        __builtin_amdgcn_sched_group_barrier(kDsRead, 2, 0);
+      }
+    }
+    float sum = weights(sc, c_in, m_run);
+    if (__ballot(!(sum <= 1048576.f))) {
+      rescale(fmaxf(m_run, row_max(sc) * c_in));
+      sum = weights(sc, c_in, m_run);
+    }
+    l_run += sum;
+    pv(vbuf(par()));
+    clear_dead(vbuf(par() ^ 1), v + 1);
+    __syncthreads();
+    ++v;
+  };
+  auto keep_b = [&] {
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt) sa[tt] = sb[tt];
+  };
+  if (!active) {  // (brings its pages; with the others' code, S^T would be live where it is not)
+    for (; v < v1; ++v) {
+      prefetch((v - v0) & 1, v);
+      clear_dead(vbuf((v - v0 + 1) & 1), v + 1);
       __syncthreads();
-      if (v + 1 < v1) load_tile(sK1, sV1, __builtin_amdgcn_readfirstlane(ahead));
-      ahead = page_of(v + 2);
-      if (active) step(sK0, sV0, v);
-      if (++v >= v1) break;
-      __syncthreads();
-      if (v + 1 < v1) load_tile(sK0, sV0, __builtin_amdgcn_readfirstlane(ahead));
-      ahead = page_of(v + 2);
-      if (active) step(sK1, sV1, v);
-      if (++v >= v1) break;
     }
   }
-  __syncthreads();  // the tile buffers become the waves' output staging
-  if (!active) return;
+  while (v < v1) {
+    if (!full(v)) {
+      if ((v - v0) & 1) step_masked(odd);
+      else step_masked(even);
+      continue;
+    }
+    const int ve = run_end(v);
+#pragma unroll
+    for (int i = 0; i < KH; ++i) qhi[i] = qhi_lds(i);
+    if ((v - v0) & 1) {
+      step_full(sa, sb, odd);
+      keep_b();
+    }
+    while (v + 1 < ve) {
+      step_full(sa, sb, even);
+      step_full(sb, sa, odd);
+    }
+    if (v < ve) {
+      step_full(sa, sb, even);
+      keep_b();
+    }
+  }
 
+  // A value that is not finite, in a tile that only some rows see, has reached rows
+  // that do not see it (0 * inf): then the item is computed again, row by row there.
+  bool bad = false;
+  {
+    float top = 0.f;
+#pragma unroll
+    for (int et = 0; et < ET; ++et)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = __builtin_elementwise_maximum(top, __builtin_fabsf(oacc[et][i]));
+    bad = !(top < INFINITY);
+  }
+  uint32_t* flags = reinterpret_cast<uint32_t*>(sK1 + kStage - 8);  // (behind the output staging)
+  const bool wave_bad = active && __ballot(bad) != 0;
+  if (l == 0) flags[w] = wave_bad;
+  __syncthreads();
+  if (flags[0] | flags[1] | flags[2] | flags[3]) {
+    m_run = -INFINITY;
+    l_run = 0.f;
+#pragma unroll
+    for (int et = 0; et < ET; ++et)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) oacc[et][i] = 0.f;
+#pragma unroll 1
+    for (int v = v0; v < v1; ++v) {
+      const int page = __builtin_amdgcn_readfirstlane(page_of(v));
+      stage(a.k_pool, sK0, page, lane_k, kStepK);
+      stage(a.v_pool, sV0, page, lane_v, kStepV);
+      __syncthreads();
+      if (active) {
+        uint32_t sees[2];
+        qk(sK0, sa, qhi_lds);
+        hide(sa, KEYS * ma_tile(kt, v), sees);
+        rescale(fmaxf(m_run, row_max(sa)));
+        l_run += weights(sa, 1.f, m_run == -INFINITY ? 0.f : m_run);
+#pragma unroll 1
+        for (int r = 0; r < 32; ++r)  // row r alone, V cleared where it sees nothing
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk) {
+            const int lane = (l & 32) + r;
+            const uint32_t see = (uint32_t)__shfl((int)sees[kk >> 1], lane, 64) >> (16 * (kk & 1));
+#pragma unroll
+            for (int et = 0; et < ET; ++et) {
+              const f32x16 o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                  __builtin_bit_cast(bf16x8, keep_bf16x8(vread(sV0, kk, et), see)), p[kk], oacc[et], 0, 0, 0);
+              if ((l & 31) == r) oacc[et] = o;
+            }
+          }
+      }
+      __syncthreads();
+    }
+  }
+
+  // The tile buffers become the waves' output staging.
+  if (active) {
   const float L = l_run + __shfl_xor(l_run, 32, 64);
   const float vsc = KV8 ? a.v_scale[c] : 1.f;
   const bool mine = xw + (l & 31) < rows;
-  if (it.nsplit > 1) {
-    const int64_t at = it.slot * ROWS + 32 * w + (l & 31);
+  if (!whole) {
+    const int64_t at = (int64_t)it.slot * ROWS + 32 * w + (l & 31);
     if (mine) {
       float* po = a.part_o + at * D + 4 * hi;
 #pragma unroll
@@ -275,8 +422,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
               f32x4{oacc[et][4 * q], oacc[et][4 * q + 1], oacc[et][4 * q + 2], oacc[et][4 * q + 3]} * vsc;
       if (hi == 0) *reinterpret_cast<float2*>(a.part_ml + at * 2) = float2{m_run, L};
     }
-    return;
-  }
+  } else {
   const float inv = L == 0.f ? 0.f : vsc / L;
   // Through LDS, so that 16 lanes store one 256-byte row.
   uint16_t* so = w == 0 ? sK0 : w == 1 ? sK1 : w == 2 ? sV0 : sV1;
@@ -304,6 +450,10 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
                                        ((int64_t)(it.row0 + ty) * a.hq + c * g + (y - ty * g)) * D + 8 * ch));
   }
   if (a.lse && hi == 0 && mine) a.lse[qrow] = (m_run + __log2f(L)) * kLn2;
+  }
+  }
+  __syncthreads();  // (the next item's tiles)
+  });
 }
 
 }  // namespace dopd

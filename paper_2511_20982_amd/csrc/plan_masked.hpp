@@ -43,14 +43,12 @@ constexpr KeyTiles ma_key_tiles(const MaskRule& m, int p0, int p1, int keys) {
 // ---- work items ---------------------------------------------------------------
 // Request r's chunk of n rows, packed with the g query heads of a KV head: packed
 // row x is token x / g, query head c * g + x % g.  An item is (request, KV head c,
-// `rows` packed rows); its tiles of keys are cut into ma_splits parts, computed by
-// different workgroups and merged exactly by log-sum-exp rescaling.
+// `rows` packed rows).
 //
 // The few-row kernel takes requests of at most kMaFewRows packed rows, the
 // many-row kernel the others; a call with both launches both.  The fp32 kernel
-// takes all and splits none.
+// takes all of them.
 constexpr int kMaFewRows = 16;
-constexpr int kMaMaxSplits = 64;
 
 enum { kMaFew = 0, kMaMany = 1, kMaF32 = 2 };
 struct MaKind {  // of a kernel: packed rows of an item, keys of a tile
@@ -74,108 +72,127 @@ constexpr int ma_most_tiles(const MaskRule& m, int pre, int n, int g, const MaKi
   const int64_t some = (int64_t)(ns + k.keys - 1) / k.keys + ((int64_t)m.window + tokens - 1 + k.keys - 1) / k.keys + 1;
   return some < whole.n ? (int)some : whole.n;
 }
-constexpr int ma_splits(int tiles, int target) {
-  return tiles <= target ? 1 : (tiles + target - 1) / target;
-}
 
-// Blocks of a request: its (KV head, split, row tile) parts, dealt so that the row
-// tiles and splits of one KV head, which read the same pages, run on one XCD (or on
-// `share` of them), with workgroup b on XCD b % xcds.  idx = split * row_tiles +
-// row tile of the part.
+// Two ways to deal a call's items to workgroups.
+//
+// Whole items: one workgroup each, the row tiles of one KV head, which read the
+// same pages, on one XCD (or on `share` of them; workgroup b is on XCD b % xcds).
 struct MaDeal {
   int xcds, share;  // share 0: in order
 };
 constexpr MaDeal ma_deal(int hkv, int xcds) {
   return hkv % xcds == 0 ? MaDeal{xcds, 1} : xcds % hkv == 0 ? MaDeal{xcds, xcds / hkv} : MaDeal{xcds, 0};
 }
-constexpr int64_t ma_blocks(const MaDeal& d, int hkv, int64_t parts) {
+constexpr int64_t ma_blocks(const MaDeal& d, int hkv, int64_t parts) {  // of a request of `parts` row tiles
   return d.share == 0 ? hkv * parts : hkv * ((parts + d.share - 1) / d.share) * d.share;
 }
-// KV head and part of block `local` of a request; false where there is none.
-constexpr bool ma_part(const MaDeal& d, int hkv, int parts, int local, int& c, int& idx) {
+// KV head and row tile of block `local` of a request; false where there is none.
+constexpr bool ma_part(const MaDeal& d, int hkv, int parts, int local, int& c, int& rt) {
   if (d.share == 0) {
     c = local / parts;
-    idx = local - c * parts;
+    rt = local - c * parts;
     return c < hkv;
   }
   const int x = local % d.xcds, k = local / d.xcds;
   if (d.share == 1) {
     c = x + d.xcds * (k / parts);
-    idx = k % parts;
+    rt = k % parts;
     return c < hkv;
   }
   c = x % hkv;
-  idx = k * d.share + x / hkv;
-  return idx < parts;
+  rt = k * d.share + x / hkv;
+  return rt < parts;
 }
+
+// Slices: an item is a span of `seg` units (the fixed cost of starting it) and one
+// per tile (ma_most_tiles of its request), the spans lie one after the other (by
+// request, KV head, row tile), and workgroup slice i takes the units
+// [i * total / nwg, (i + 1) * total / nwg): equal work whatever the lengths, one
+// round over the machine.  An item whose tiles lie in several slices leaves a
+// partial result in each: in slot 2 i where its part starts with the slice (or
+// earlier), else in slot 2 i + 1.  Consecutive slices run on one XCD.
+constexpr int64_t ma_slice_begin(int64_t i, int64_t total, int64_t nwg) { return i * total / nwg; }
+constexpr int64_t ma_slice_of(int64_t unit, int64_t total, int64_t nwg) {
+  int64_t i = unit * nwg / total;
+  while (i + 1 < nwg && ma_slice_begin(i + 1, total, nwg) <= unit) ++i;
+  while (i > 0 && ma_slice_begin(i, total, nwg) > unit) --i;
+  return i;
+}
+constexpr int ma_slice_index(int b, int nwg, int xcds) {
+  return nwg % xcds == 0 ? b % xcds * (nwg / xcds) + b / xcds : b;
+}
+constexpr int64_t ma_span_units(const MaskRule& m, int pre, int n, int g, const MaKind& k, int seg) {
+  return seg + ma_most_tiles(m, pre, n, g, k);
+}
+constexpr int64_t kMaMaxUnits = INT32_MAX / 2;
 
 // ---- a call's plan --------------------------------------------------------------
 struct MaPlan {
-  int target;          // tiles of a part
-  int64_t blocks;      // workgroups
-  int64_t slots;       // partial results (0: nothing is split)
-  int64_t merges;      // items that are merged
+  int64_t blocks;  // workgroups (0: no item)
+  int nwg;         // slices (0: whole items)
+  int seg;
+  int64_t total;   // units
+  bool fits;       // the counts fit the kernels' integers
 };
 
-// The target that a simple model of the call makes fastest: with as many resident
-// workgroups as `resident`, parts of at most `target` tiles that each cost `start`
-// tiles more to begin and to merge, all rounds but the last full.
-inline MaPlan ma_plan_of(const MaskRule& m, const MaKind& k, const int32_t* cu, const int32_t* pre, int nreq, int g,
-                         int hkv, const MaDeal& d, int target) {
-  MaPlan p{target, 0, 0, 0};
+struct MaCosts {
+  int seg;         // start of an item, in tiles
+  int merge;       // of a sliced call, in tiles: the partials and the kernel that merges them
+  int min_tiles;   // fewest units of a slice
+};
+
+// Tiles that a request's items have on average (windows: the first rows of a
+// context see less than the others).
+inline double ma_mean_tiles(const MaskRule& m, int pre, int n, int g, const MaKind& k) {
+  const double most = ma_most_tiles(m, pre, n, g, k);
+  if (m.tree || pre + 1 >= m.window) return most;
+  const double first = (pre + 1 + k.keys - 1) / k.keys;
+  const double grow = std::min<double>(n, m.window - pre);  // rows until the window is full
+  return most - (most - std::min(first, most)) * 0.5 * grow / n;
+}
+
+// Whole items where they fill the machine evenly enough, else slices: with R
+// workgroups resident, whole items take about their tiles and starts over R plus
+// half the longest item (the last round), and at least the longest; slices take the
+// same over R and the merge.
+inline MaPlan ma_plan(const MaskRule& m, const MaKind& k, const int32_t* cu, const int32_t* pre, int nreq, int g,
+                      int hkv, const MachineShape& mach, const MaCosts& cost) {
+  const int xcds = std::max(1, mach.xcds);
+  const MaDeal d = ma_deal(hkv, xcds);
+  const double resident = (double)kWgPerCu * std::max(1, mach.cus);
+  MaPlan p{0, 0, cost.seg, 0, true};
+  double items = 0, work = 0, bound = 0, longest = 0;
   for (int r = 0; r < nreq; ++r) {
     const int n = cu[r + 1] - cu[r];
     if (!ma_mine(k, n, g)) continue;
-    const int rt = ma_row_tiles(n, g, k.rows), s = ma_splits(ma_most_tiles(m, pre[r], n, g, k), target);
-    p.blocks += ma_blocks(d, hkv, (int64_t)rt * s);
-    if (s > 1) {
-      p.slots += (int64_t)hkv * rt * s;
-      p.merges += (int64_t)hkv * rt;
-    }
+    const int rt = ma_row_tiles(n, g, k.rows);
+    const double most = ma_most_tiles(m, pre[r], n, g, k), all = (double)hkv * rt;
+    p.blocks += ma_blocks(d, hkv, rt);
+    p.total += (int64_t)hkv * rt * ma_span_units(m, pre[r], n, g, k, cost.seg);
+    items += all;
+    work += all * (ma_mean_tiles(m, pre[r], n, g, k) + cost.seg);
+    bound += all * (most + cost.seg);
+    longest = std::max(longest, most + cost.seg);
   }
+  if (p.blocks == 0) return p;
+  const double whole = items <= resident ? longest : std::max(longest, work / resident + 0.5 * longest);
+  const double slices = std::min(resident, std::max(1.0, bound / cost.min_tiles));
+  const double sliced = (bound + slices * cost.seg) / slices + cost.merge;
+  p.fits = p.blocks <= kMaMaxUnits && p.total <= kMaMaxUnits;
+  if (k.which == kMaF32 || whole <= sliced || !p.fits) return p;
+  p.nwg = (int)slices;
+  if (p.nwg > xcds) p.nwg -= p.nwg % xcds;
+  p.blocks = p.nwg;
   return p;
 }
 
-inline MaPlan ma_plan(const MaskRule& m, const MaKind& k, const int32_t* cu, const int32_t* pre, int nreq, int g,
-                      int hkv, const MachineShape& mach, int min_tiles, int start) {
-  const MaDeal d = ma_deal(hkv, std::max(1, mach.xcds));
-  int most = 0;
-  for (int r = 0; r < nreq; ++r)
-    if (ma_mine(k, cu[r + 1] - cu[r], g)) most = std::max(most, ma_most_tiles(m, pre[r], cu[r + 1] - cu[r], g, k));
-  if (most == 0) return MaPlan{1, 0, 0, 0};
-  const int64_t resident = (int64_t)kWgPerCu * std::max(1, mach.cus);
-  int best = most;
-  double least = -1;
-  for (int s = 1; s <= kMaMaxSplits; s = s < 4 ? s + 1 : s + s / 2) {
-    const int target = (most + s - 1) / s;
-    if (s > 1 && target < min_tiles) break;
-    double items = 0, tiles = 0;
-    for (int r = 0; r < nreq; ++r) {
-      const int n = cu[r + 1] - cu[r];
-      if (!ma_mine(k, n, g)) continue;
-      const int t = ma_most_tiles(m, pre[r], n, g, k);
-      const double it = (double)hkv * ma_row_tiles(n, g, k.rows);
-      items += it * ma_splits(t, target);
-      tiles += it * t;
-    }
-    const double longest = target + start;
-    const double each = (tiles + items * start) / (double)resident;
-    const double time = items <= (double)resident ? longest : each + 0.5 * longest;
-    if (least < 0 || time < least) {
-      least = time;
-      best = target;
-    }
-  }
-  return ma_plan_of(m, k, cu, pre, nreq, g, hkv, d, best);
-}
-
-// Workspace of one kernel's plan: [slots][rows][D] partial outputs, then
-// [slots][rows][2] (m, l), each at a multiple of 256 bytes.
+// Workspace of one kernel's plan: [2 nwg][rows][D] partial outputs, then
+// [2 nwg][rows][2] (m, l), each at a multiple of 256 bytes.
 inline size_t ma_part_ml_off(const MaPlan& p, const MaKind& k, int d) {
-  return align256((size_t)p.slots * k.rows * d * sizeof(float));
+  return align256((size_t)2 * p.nwg * k.rows * d * sizeof(float));
 }
 inline size_t ma_ws_bytes(const MaPlan& p, const MaKind& k, int d) {
-  return p.slots == 0 ? 0 : ma_part_ml_off(p, k, d) + align256((size_t)p.slots * k.rows * 2 * sizeof(float));
+  return p.nwg <= 1 ? 0 : ma_part_ml_off(p, k, d) + align256((size_t)2 * p.nwg * k.rows * 2 * sizeof(float));
 }
 
 }  // namespace dopd

@@ -1,13 +1,14 @@
 // CPU check of the planning of the windowed and the tree attention
 // (paper_2511_20982_amd/csrc/plan_masked.hpp): the visited tiles hold every position
 // a row sees, the pages read are pages that some row sees, the workgroups of a plan
-// cover every part of every item once, and their partial slots are distinct.
+// take every tile of every item once, and the merge reads the partials they leave.
 // Usage: masked_harness <cus> <xcds> <cases>; prints "ok" or the first failure.
 #include <cstdio>
 #include <cstdlib>
+#include <map>
 #include <random>
 #include <set>
-#include <tuple>
+#include <utility>
 #include <vector>
 
 #include "../paper_2511_20982_amd/csrc/plan_masked.hpp"
@@ -64,45 +65,104 @@ static int check_tiles(const MaskRule& m, int pre, int n, int g, const MaKind& k
   return 0;
 }
 
+// Walks the workgroups of a plan as the kernels do: every tile of every item is taken
+// once, partial results lie in slots of their own, and the merge finds each split
+// item once, with the slots that were written.
 static int check_plan(const MaskRule& m, const std::vector<int32_t>& cu, const std::vector<int32_t>& pre, int g,
-                      int hkv, const MaKind& k, const MachineShape& mach) {
+                      int hkv, const MaKind& k, const MachineShape& mach, const MaCosts& cost, bool slices) {
   const int n = (int)pre.size();
   const MaDeal d = ma_deal(hkv, mach.xcds);
-  const MaPlan p = ma_plan(m, k, cu.data(), pre.data(), n, g, hkv, mach, 4, 3);
-  int64_t base = 0, slot0 = 0, merges = 0;
-  std::set<std::tuple<int, int, int>> seen;
-  std::set<int64_t> slots;
+  MaPlan p = ma_plan(m, k, cu.data(), pre.data(), n, g, hkv, mach, cost);
+  if (!p.fits) return fail("does not fit", p.blocks, p.total);
+  if (slices && p.nwg == 0 && p.blocks > 0) p.blocks = p.nwg = 1 + (int)(p.total % 97);  // (any count has to work)
+  struct Item {
+    int r, c, rt, tiles;
+    int64_t first;
+  };
+  std::vector<Item> items;
+  int64_t units = 0, base = 0;
   for (int r = 0; r < n; ++r) {
     const int len = cu[r + 1] - cu[r];
     if (!ma_mine(k, len, g)) continue;
-    const int rt = ma_row_tiles(len, g, k.rows), s = ma_splits(ma_most_tiles(m, pre[r], len, g, k), p.target);
-    if (s > kMaMaxSplits * 2) return fail("splits", s, p.target);
-    const int parts = rt * s;
-    const int64_t blocks = ma_blocks(d, hkv, parts);
-    if (d.share && (blocks % mach.xcds || base % mach.xcds)) return fail("XCD phase", blocks, base);
-    for (int64_t b = 0; b < blocks; ++b) {
-      int c, idx;
-      if (!ma_part(d, hkv, parts, (int)b, c, idx)) continue;
-      if (c < 0 || c >= hkv || idx < 0 || idx >= parts) return fail("part out of range", c, idx);
-      if (!seen.insert({r, c, idx}).second) return fail("part dealt twice", r, idx);
-      if (s > 1 && !slots.insert(slot0 + (int64_t)c * parts + idx).second) return fail("slot used twice", r, idx);
+    const int rts = ma_row_tiles(len, g, k.rows);
+    for (int c = 0; c < hkv; ++c)
+      for (int rt = 0; rt < rts; ++rt) {
+        const int p0 = pre[r] + rt * k.rows / g, p1 = pre[r] + (std::min(len * g, (rt + 1) * k.rows) - 1) / g;
+        items.push_back({r, c, rt, ma_key_tiles(m, p0, m.tree ? pre[r] + len - 1 : p1, k.keys).n, units});
+        units += ma_span_units(m, pre[r], len, g, k, p.seg);
+      }
+    const int64_t blocks = ma_blocks(d, hkv, rts);
+    if (p.nwg == 0) {
+      if (d.share && (blocks % mach.xcds || base % mach.xcds)) return fail("XCD phase", blocks, base);
+      std::set<std::pair<int, int>> seen;
+      for (int64_t b = 0; b < blocks; ++b) {
+        int c, rt;
+        if (!ma_part(d, hkv, rts, (int)b, c, rt)) continue;
+        if (c < 0 || c >= hkv || rt < 0 || rt >= rts) return fail("item out of range", c, rt);
+        if (!seen.insert({c, rt}).second) return fail("item dealt twice", r, rt);
+      }
+      if ((int)seen.size() != hkv * rts) return fail("items missing", (long)seen.size(), hkv * rts);
     }
-    if ((int64_t)seen.size() == 0) return fail("no part", r, parts);
     base += blocks;
-    if (s > 1) {
-      slot0 += (int64_t)hkv * parts;
-      merges += (int64_t)hkv * rt;
+  }
+  if (units != p.total) return fail("units", units, p.total);
+  if (p.nwg == 0) return base == p.blocks ? 0 : fail("blocks", base, p.blocks);
+  std::set<int> order;
+  for (int b = 0; b < p.nwg; ++b) order.insert(ma_slice_index(b, p.nwg, mach.xcds));
+  if ((int)order.size() != p.nwg || *order.begin() != 0 || *order.rbegin() != p.nwg - 1) return fail("slice order", p.nwg, 0);
+  std::map<std::pair<size_t, int>, int> written;  // (item, slice) -> slot
+  std::set<int> slots;
+  std::vector<int> taken(items.size(), 0);
+  size_t at = 0;
+  for (int i = 0; i < p.nwg; ++i) {
+    const int64_t begin = ma_slice_begin(i, p.total, p.nwg), end = ma_slice_begin(i + 1, p.total, p.nwg);
+    if (begin > end || (i == 0 && begin != 0) || (i == p.nwg - 1 && end != p.total)) return fail("slices", begin, end);
+    int64_t pos = begin;
+    while (at > 0 && items[at].first > pos) --at;
+    while (at + 1 < items.size() && items[at + 1].first <= pos) ++at;
+    while (pos < end) {
+      const Item& it = items[at];
+      const int len = cu[it.r + 1] - cu[it.r];
+      const int span = (int)ma_span_units(m, pre[it.r], len, g, k, p.seg), u0 = (int)(pos - it.first);
+      const int u1 = (int)std::min<int64_t>(span, u0 + end - pos);
+      const int v0 = std::min(it.tiles, std::max(0, u0 - p.seg)), v1 = std::min(it.tiles, u1 - p.seg);
+      if (u1 > p.seg && v0 < v1) {
+        if (v0 != taken[at]) return fail("tiles out of order", v0, taken[at]);
+        taken[at] = v1;
+        if (!(v0 == 0 && v1 == it.tiles)) {
+          const int slot = 2 * i + (pos == begin ? 0 : 1);
+          if (!slots.insert(slot).second || slot >= 2 * p.nwg) return fail("slot", slot, p.nwg);
+          written[{at, i}] = slot;
+        }
+      }
+      pos += u1 - u0;
+      if (pos < end || pos == it.first + span) {
+        if (pos == it.first + span && at + 1 < items.size()) ++at;
+      }
     }
   }
-  int64_t want = 0;
-  for (int r = 0; r < n; ++r) {
-    const int len = cu[r + 1] - cu[r];
-    if (ma_mine(k, len, g))
-      want += (int64_t)hkv * ma_row_tiles(len, g, k.rows) * ma_splits(ma_most_tiles(m, pre[r], len, g, k), p.target);
+  for (size_t i = 0; i < items.size(); ++i)
+    if (taken[i] != items[i].tiles) return fail("tiles missing", taken[i], items[i].tiles);
+  std::set<size_t> merged;
+  size_t found = 0;
+  for (int slice = 1; slice < p.nwg; ++slice) {
+    const int64_t unit = ma_slice_begin(slice, p.total, p.nwg);
+    if (unit >= p.total) continue;
+    size_t i = 0;
+    while (i + 1 < items.size() && items[i + 1].first <= unit) ++i;
+    const Item& it = items[i];
+    const int b0 = (int)ma_slice_of(it.first + p.seg, p.total, p.nwg);
+    const int b1 = (int)ma_slice_of(it.first + p.seg + it.tiles - 1, p.total, p.nwg);
+    if (b0 == b1 || slice != b0 + 1) continue;
+    if (!merged.insert(i).second) return fail("merged twice", i, slice);
+    for (int b = b0; b <= b1; ++b) {
+      const int slot = b == b0 ? 2 * b0 + (ma_slice_begin(b0, p.total, p.nwg) >= it.first ? 0 : 1) : 2 * b;
+      auto w = written.find({i, b});
+      if (w == written.end() || w->second != slot) return fail("merge reads a slot that was not written", b, slot);
+      ++found;
+    }
   }
-  if ((int64_t)seen.size() != want) return fail("parts missing", (long)seen.size(), want);
-  if (base != p.blocks || slot0 != p.slots || merges != p.merges) return fail("totals", base, p.blocks);
-  if (!slots.empty() && *slots.rbegin() >= p.slots) return fail("slot past the workspace", *slots.rbegin(), p.slots);
+  if (found != written.size()) return fail("partials not merged", found, (long)written.size());
   return 0;
 }
 
@@ -128,16 +188,18 @@ int main(int argc, char** argv) {
       cu.push_back(cu.back() + (pick(0, 3) ? log(0, 300) : pick(0, 2)));
       pre.push_back(pick(0, 4) ? log(0, 900) : pick(0, 100000));
     }
-    for (int which : {(int)kMaFew, (int)kMaMany})
-      if (int rc = check_plan(m, cu, pre, g, hkv, ma_kind(which), mach)) return rc;
+    const MaCosts cost{pick(0, 12), pick(0, 20), pick(1, 6)};
+    for (int which : {(int)kMaFew, (int)kMaMany, (int)kMaF32})
+      for (bool slices : {false, true})
+        if (int rc = check_plan(m, cu, pre, g, hkv, ma_kind(which), mach, cost, slices && which != kMaF32)) return rc;
   }
   // Positions and windows at their limits do not overflow.
   for (int which : {(int)kMaFew, (int)kMaMany, (int)kMaF32}) {
     const MaKind k = ma_kind(which);
     const int32_t cu[2] = {0, which == kMaFew ? 1 : 17}, pre[1] = {kMaMaxPos - 17};
     for (const MaskRule m : {MaskRule{1, 0, 0}, MaskRule{0, kMaMaxPos, kMaMaxPos}, MaskRule{0, 1, 0}}) {
-      const MaPlan p = ma_plan(m, k, cu, pre, 1, 1, 8, mach, 4, 3);
-      if (which != kMaF32 && (p.blocks < 8 || p.slots < 0)) return fail("largest positions", p.blocks, p.slots);
+      const MaPlan p = ma_plan(m, k, cu, pre, 1, 1, 8, mach, MaCosts{3, 6, 3});
+      if (p.blocks < 8 || p.total < 8) return fail("largest positions", p.blocks, p.total);
     }
   }
   std::printf("ok\n");
