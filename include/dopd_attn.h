@@ -497,8 +497,9 @@ size_t dopd_pd_step_workspace_size(const dopd_attn_shape* shape,
  *     exactly, by log-sum-exp rescaling, on the same stream).  May be null when
  *     that needs none.  Calls that overlap in time must not share it.
  *   lse (nullable): fp32 [T][Hq].
- * Requests of at most 16 rows times Hq / Hkv run one kernel, the others another;
- * a call that holds both launches both.  Any Hq / Hkv.  q, out and the pools are
+ * Requests of at most 16, at most 64 and more rows times Hq / Hkv run three kernels;
+ * a call that holds several sizes launches several, or takes a few small ones into the
+ * kernel of the larger.  Any Hq / Hkv.  q, out and the pools are
  * 16-byte aligned, prefix_lens[r] + n_r is at most 2^30, and
  * n_r * (Hq / Hkv)^2 < 2^32 (DOPD_ERR_INVALID_SHAPE otherwise).
  * bf16: products of bf16 operands with fp32 accumulation, weights rounded to bf16

@@ -7,6 +7,7 @@
 #include "kernels/masked_common.hpp"
 #include "kernels/masked_f32.hpp"
 #include "kernels/masked_few.hpp"
+#include "kernels/masked_mid.hpp"
 #include "kernels/masked_rows.hpp"
 #include "plan_masked.hpp"
 
@@ -42,20 +43,23 @@ dopd::MaskRule window_rule(int32_t window, int32_t sinks) {
 }
 dopd::MaskRule tree_rule() { return dopd::MaskRule{1, 0, 0}; }
 
-dopd::MaPlan masked_plan(int which, const dopd_attn_shape* s, const dopd::MaskRule& rule, const int32_t* cu_host,
-                         const int32_t* prefix_host, int32_t nreq) {
-  const dopd::MaCosts cost = which == dopd::kMaFew ? dopd::MaCosts{s->dtype == DOPD_FP8_E4M3 ? 12 : 8, 16, 4}
-                                                   : dopd::MaCosts{3, 6, 3};
+dopd::MaPlan masked_plan(const dopd::MaKind& k, const dopd_attn_shape* s, const dopd::MaskRule& rule,
+                         const int32_t* cu_host, const int32_t* prefix_host, int32_t nreq) {
+  const dopd::MaCosts cost = k.which == dopd::kMaMany ? dopd::MaCosts{3, 6, 3}
+                                                      : dopd::MaCosts{s->dtype == DOPD_FP8_E4M3 ? 12 : 8, 16, 4};
   const int g = s->num_q_heads / s->num_kv_heads;
-  return dopd::ma_plan(rule, dopd::ma_kind(which), cu_host, prefix_host, nreq, g, s->num_kv_heads, machine_shape(), cost);
+  return dopd::ma_plan(rule, k, cu_host, prefix_host, nreq, g, s->num_kv_heads, machine_shape(), cost);
 }
 
 size_t masked_ws_bytes(const dopd_attn_shape* s, const dopd::MaskRule& rule, const int32_t* cu_host,
                        const int32_t* prefix_host, int32_t nreq) {
   if (s->dtype == DOPD_FP32) return 0;
+  const dopd::MaSplit split = dopd::ma_split(rule, cu_host, prefix_host, nreq, s->num_q_heads / s->num_kv_heads);
   size_t bytes = 0;
-  for (int which : {dopd::kMaFew, dopd::kMaMany})
-    bytes += dopd::ma_ws_bytes(masked_plan(which, s, rule, cu_host, prefix_host, nreq), dopd::ma_kind(which), s->head_dim);
+  for (int i = 0; i < 3; ++i) {
+    const dopd::MaKind k = dopd::ma_kernel(split, i);
+    bytes += dopd::ma_ws_bytes(masked_plan(k, s, rule, cu_host, prefix_host, nreq), k, s->head_dim);
+  }
   return bytes;
 }
 
@@ -67,22 +71,26 @@ size_t masked_workspace_size(const dopd_attn_shape* s, const dopd::MaskRule& rul
 }
 
 template <int D, bool KV8, bool TREE>
-dopd_status launch_masked(int which, const dopd::MaskedArgs& a, const dopd::MaPlan& p, hipStream_t strm) {
-  const dim3 grid = grid_of(p.blocks), block(256);
-  if (which == dopd::kMaFew) hipLaunchKernelGGL((dopd::masked_few_kernel<D, KV8, TREE>), grid, block, 0, strm, a);
-  else hipLaunchKernelGGL((dopd::masked_rows_kernel<D, KV8, TREE>), grid, block, 0, strm, a);
+dopd_status launch_masked(const dopd::MaKind& k, const dopd::MaskedArgs& a, const dopd::MaPlan& p, hipStream_t strm) {
+  const dim3 grid = grid_of(p.blocks), block(256), merge((unsigned)((p.nwg - 1) * (k.rows / dopd::merge_rows<D>())));
+  switch (k.which) {
+    case dopd::kMaFew: hipLaunchKernelGGL((dopd::masked_few_kernel<D, KV8, TREE>), grid, block, 0, strm, a); break;
+    case dopd::kMaMid: hipLaunchKernelGGL((dopd::masked_mid_kernel<D, KV8, TREE>), grid, block, 0, strm, a); break;
+    default: hipLaunchKernelGGL((dopd::masked_rows_kernel<D, KV8, TREE>), grid, block, 0, strm, a);
+  }
   const dopd_status st = launch_status();
   if (st != DOPD_OK || p.nwg <= 1) return st;
-  if (which == dopd::kMaFew)
-    hipLaunchKernelGGL((dopd::masked_merge_kernel<D, dopd::kMaFew, TREE>), dim3((unsigned)(p.nwg - 1)), block, 0, strm, a);
-  else
-    hipLaunchKernelGGL((dopd::masked_merge_kernel<D, dopd::kMaMany, TREE>), dim3((unsigned)(8 * (p.nwg - 1))), block, 0, strm, a);
+  switch (k.which) {
+    case dopd::kMaFew: hipLaunchKernelGGL((dopd::masked_merge_kernel<D, dopd::kMaFew>), merge, block, 0, strm, a); break;
+    case dopd::kMaMid: hipLaunchKernelGGL((dopd::masked_merge_kernel<D, dopd::kMaMid>), merge, block, 0, strm, a); break;
+    default: hipLaunchKernelGGL((dopd::masked_merge_kernel<D, dopd::kMaMany>), merge, block, 0, strm, a);
+  }
   return launch_status();
 }
 
 template <bool KV8, bool TREE>
-dopd_status launch_masked_d(int which, const dopd::MaskedArgs& a, const dopd::MaPlan& p, int d, hipStream_t strm) {
-  return d == 64 ? launch_masked<64, KV8, TREE>(which, a, p, strm) : launch_masked<128, KV8, TREE>(which, a, p, strm);
+dopd_status launch_masked_d(const dopd::MaKind& k, const dopd::MaskedArgs& a, const dopd::MaPlan& p, int d, hipStream_t strm) {
+  return d == 64 ? launch_masked<64, KV8, TREE>(k, a, p, strm) : launch_masked<128, KV8, TREE>(k, a, p, strm);
 }
 
 dopd_status masked_impl(const dopd_attn_shape* s, bool kv8, const void* q, const void* k_pool, const void* v_pool,
@@ -133,6 +141,7 @@ dopd_status masked_impl(const dopd_attn_shape* s, bool kv8, const void* q, const
   if (s->dtype == DOPD_FP32) {
     const dopd::MaKind kind = dopd::ma_kind(dopd::kMaF32);
     a.scale = s->softmax_scale;
+    a.hi = INT32_MAX;
     const dopd::MaPlan p = dopd::ma_plan(rule, kind, cu_host, prefix_host, nreq, hq / hkv, hkv, machine_shape(), dopd::MaCosts{});
     if (!p.fits) return DOPD_ERR_INVALID_SHAPE;
     const dim3 grid = grid_of(p.blocks);
@@ -149,12 +158,14 @@ dopd_status masked_impl(const dopd_attn_shape* s, bool kv8, const void* q, const
   }
 
   a.scale = s->softmax_scale * dopd::kLog2e;
-  dopd::MaPlan plans[2];
+  const dopd::MaSplit split = dopd::ma_split(rule, cu_host, prefix_host, nreq, hq / hkv);
+  dopd::MaPlan plans[3];
   size_t need = 0;
-  for (int which : {dopd::kMaFew, dopd::kMaMany}) {
-    plans[which] = masked_plan(which, s, rule, cu_host, prefix_host, nreq);
-    if (!plans[which].fits) return DOPD_ERR_INVALID_SHAPE;
-    need += dopd::ma_ws_bytes(plans[which], dopd::ma_kind(which), d);
+  for (int i = 0; i < 3; ++i) {
+    const dopd::MaKind k = dopd::ma_kernel(split, i);
+    plans[i] = masked_plan(k, s, rule, cu_host, prefix_host, nreq);
+    if (!plans[i].fits) return DOPD_ERR_INVALID_SHAPE;
+    need += dopd::ma_ws_bytes(plans[i], k, d);
   }
   if (need > 0) {
     if (!workspace) return DOPD_ERR_NULL_POINTER;
@@ -162,18 +173,21 @@ dopd_status masked_impl(const dopd_attn_shape* s, bool kv8, const void* q, const
   }
   if ((reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return DOPD_ERR_INVALID_SHAPE;
   char* ws = static_cast<char*>(workspace);
-  for (int which : {dopd::kMaMany, dopd::kMaFew}) {  // (the longer kernel first)
-    const dopd::MaPlan& p = plans[which];
+  for (int i = 2; i >= 0; --i) {  // (the longest kernel first)
+    const dopd::MaPlan& p = plans[i];
     if (p.blocks == 0) continue;
-    const dopd::MaKind kind = dopd::ma_kind(which);
+    const dopd::MaKind k = dopd::ma_kernel(split, i);
+    a.lo = k.lo;
+    a.hi = k.hi;
     a.nwg = p.nwg;
     a.seg = p.seg;
     a.total = (int)p.total;
+    a.slices = dopd::ma_slices(p.total, p.nwg);
     a.part_o = reinterpret_cast<float*>(ws);
-    a.part_ml = reinterpret_cast<float*>(ws + dopd::ma_part_ml_off(p, kind, d));
-    ws += dopd::ma_ws_bytes(p, kind, d);
-    if (kv8) st = rule.tree ? launch_masked_d<true, true>(which, a, p, d, strm) : launch_masked_d<true, false>(which, a, p, d, strm);
-    else st = rule.tree ? launch_masked_d<false, true>(which, a, p, d, strm) : launch_masked_d<false, false>(which, a, p, d, strm);
+    a.part_ml = reinterpret_cast<float*>(ws + dopd::ma_part_ml_off(p, k, d));
+    ws += dopd::ma_ws_bytes(p, k, d);
+    if (kv8) st = rule.tree ? launch_masked_d<true, true>(k, a, p, d, strm) : launch_masked_d<true, false>(k, a, p, d, strm);
+    else st = rule.tree ? launch_masked_d<false, true>(k, a, p, d, strm) : launch_masked_d<false, false>(k, a, p, d, strm);
     if (st != DOPD_OK) return st;
   }
   return DOPD_OK;

@@ -37,6 +37,8 @@ struct MaskedArgs {
   FastDiv by_g;               // (packed rows of a call stay below 2^32 / g: host check)
   int pt_stride, nreq, hq, hkv, words;
   int nwg, seg, total;        // slices (nwg 0: whole items), see the plan
+  MaSlices slices;
+  int lo, hi;                 // packed rows of the requests that this kernel takes: in (lo, hi]
   float scale;                // softmax scale, times log2(e) but for fp32
 };
 
@@ -78,6 +80,45 @@ __device__ __forceinline__ int seen_page(const MaskedArgs& a, int t, int low_key
   return t * kPage >= a.rule.sinks && t < low ? low : min(t, (end - 1) / kPage);
 }
 
+// Eight bf16 (or E4M3 codes), of which those with a set bit are kept.
+__device__ __forceinline__ u32x4 keep_of(u32x4 x, uint32_t bits) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    x[i] &= (bits >> (2 * i) & 1u ? 0xffffu : 0u) | (bits >> (2 * i) & 2u ? 0xffff0000u : 0u);
+  return x;
+}
+__device__ __forceinline__ u32x2 keep_of(u32x2 x, uint32_t bits) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t b = bits >> (4 * i);
+    x[i] &= (b & 1u ? 0xffu : 0u) | (b & 2u ? 0xff00u : 0u) | (b & 4u ? 0xff0000u : 0u) | (b & 8u ? 0xff000000u : 0u);
+  }
+  return x;
+}
+
+// Eight keys of a V row as a bf16 operand.
+__device__ __forceinline__ bf16x8 v_operand(u32x4 v) { return __builtin_bit_cast(bf16x8, v); }
+__device__ __forceinline__ bf16x8 v_operand(u32x2 v) {
+  const u32x2 lo = bf16x4_from_e4m3x4(v[0]), hi = bf16x4_from_e4m3x4(v[1]);
+  return __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
+}
+
+__device__ __forceinline__ void store_bf16x4(void* out, int64_t at, f32x4 o) {
+  u32x2 w;
+  w[0] = pack_bf16x2(o[0], o[1]);
+  w[1] = pack_bf16x2(o[2], o[3]);
+  *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(out) + at) = w;
+}
+template <int N, class V>
+__device__ __forceinline__ bool any_not_finite(const V (&o)[N]) {  // in the wave
+  float top = 0.f;
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (unsigned j = 0; j < sizeof(V) / 4; ++j) top = __builtin_elementwise_maximum(top, __builtin_fabsf(o[n][j]));
+  return __ballot(!(top < INFINITY)) != 0;
+}
+
 // A workgroup's item, or the part of one that lies in its slice.
 struct MaItem {
   int req, c, rt;
@@ -91,7 +132,7 @@ struct MaItem {
 // part.  false: past the last one.
 template <int KIND, class Count>
 __device__ __forceinline__ bool ma_find(const MaskedArgs& a, int x, Count count, MaItem& it, int& local) {
-  constexpr MaKind kind = ma_kind(KIND);
+  const MaKind kind = ma_kind(KIND, a.lo, a.hi);
   const int l = lane_id(), g = (int)a.by_g.d;
   int base = 0;
   for (int r0 = 0; r0 < a.nreq; r0 += 64) {
@@ -117,7 +158,7 @@ __device__ __forceinline__ bool ma_find(const MaskedArgs& a, int x, Count count,
 // Calls body(item) for each item of workgroup b (uniform).
 template <int KIND, class Body>
 __device__ __forceinline__ void ma_items(const MaskedArgs& a, int b, Body body) {
-  constexpr MaKind kind = ma_kind(KIND);
+  const MaKind kind = ma_kind(KIND, a.lo, a.hi);
   const int g = (int)a.by_g.d;
   MaItem it;
   int local, begin = 0, pos = 0, end = 0, slice = 0;
@@ -130,8 +171,8 @@ __device__ __forceinline__ void ma_items(const MaskedArgs& a, int b, Body body) 
     if (!ma_part(a.deal, a.hkv, ma_row_tiles(it.n, g, kind.rows), local, it.c, it.rt)) return;
   } else {
     slice = ma_slice_index(b, a.nwg, a.deal.xcds);
-    begin = pos = (int)ma_slice_begin(slice, a.total, a.nwg);
-    end = (int)ma_slice_begin(slice + 1, a.total, a.nwg);
+    begin = pos = ma_slice_begin(slice, a.slices);
+    end = ma_slice_begin(slice + 1, a.slices);
     if (pos >= end || !ma_find<KIND>(a, pos, units, it, local)) return;
   }
   while (true) {  // slices: one item, or part of one, at a time
@@ -168,21 +209,22 @@ __device__ __forceinline__ bool ma_tiles_of(const MaskedArgs& a, const MaItem& i
   return v0 == 0 && v1 == n;
 }
 
-// The merge of the items that lie in several slices: workgroup = 16 packed rows of
-// the item that slice 1 + blockIdx.x / (rows / 16) continues, if that slice is the
-// first to continue it; thread = a 4-dim chunk of a row, the partials folded in key
-// order:
+// The merge of the items that lie in several slices: workgroup = merge_rows packed
+// rows of the item that a slice continues, if that slice is the first to continue it;
+// thread = a 4-dim chunk of a row, the partials folded in key order:
 //   M = max_s m_s,  L = sum_s 2^(m_s - M) l_s,  o = sum_s 2^(m_s - M) o~_s / L.
 // Bound by the partials' bytes and the start of a kernel.
-template <int D, int KIND, bool TREE>
+template <int D>
+constexpr int merge_rows() { return 256 / (D / 4); }
+template <int D, int KIND>
 __global__ __launch_bounds__(256) void masked_merge_kernel(MaskedArgs a) {
-  constexpr MaKind kind = ma_kind(KIND);
-  constexpr int ROWS = kind.rows, kGroup = 16, CH = D / 4;
+  const MaKind kind = ma_kind(KIND, a.lo, a.hi);
+  constexpr int ROWS = ma_kind(KIND).rows, kGroup = merge_rows<D>(), CH = D / 4;
   const int g = (int)a.by_g.d;
   const int slice = 1 + (int)blockIdx.x / (ROWS / kGroup), group = (int)blockIdx.x % (ROWS / kGroup);
   MaItem it;
   int local;
-  const int at = (int)ma_slice_begin(slice, a.total, a.nwg);
+  const int at = ma_slice_begin(slice, a.slices);
   auto units = [&](int n, int pre) {
     return a.hkv * ma_row_tiles(n, g, ROWS) * (int)ma_span_units(a.rule, pre, n, g, kind, a.seg);
   };
@@ -192,15 +234,13 @@ __global__ __launch_bounds__(256) void masked_merge_kernel(MaskedArgs a) {
   const int x0 = rt * ROWS, live = min(ROWS, it.n * g - x0);
   if (group * kGroup >= live) return;
   const int p0 = it.pre + fast_quot(x0, a.by_g), p1 = it.pre + fast_quot(x0 + live - 1, a.by_g);
-  const int tiles = ma_key_tiles(a.rule, p0, TREE ? it.pre + it.n - 1 : p1, kind.keys).n;
+  const int tiles = ma_key_tiles(a.rule, p0, a.rule.tree ? it.pre + it.n - 1 : p1, kind.keys).n;
   const int first = at - (local - index * span);  // the item's first unit
-  const int b0 = (int)ma_slice_of(first + a.seg, a.total, a.nwg);
-  const int b1 = (int)ma_slice_of(first + a.seg + tiles - 1, a.total, a.nwg);
+  const int b0 = ma_slice_of(first + a.seg, a.slices), b1 = ma_slice_of(first + a.seg + tiles - 1, a.slices);
   if (b0 == b1 || slice != b0 + 1) return;
-  const int slot0 = 2 * b0 + (ma_slice_begin(b0, a.total, a.nwg) >= first ? 0 : 1);
-  for (int i = (int)threadIdx.x; i < kGroup * CH; i += 256) {
-    const int row = kGroup * group + i / CH, e0 = 4 * (i % CH);
-    if (row >= live) break;
+  const int slot0 = 2 * b0 + (ma_slice_begin(b0, a.slices) >= first ? 0 : 1);
+  const int row = kGroup * group + (int)threadIdx.x / CH, e0 = 4 * ((int)threadIdx.x % CH);
+  if (row < live) {
     float M = -INFINITY, L = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     for (int b = b0; b <= b1; b += 4) {  // four partials in flight
@@ -225,10 +265,7 @@ __global__ __launch_bounds__(256) void masked_merge_kernel(MaskedArgs a) {
     const float inv = L == 0.f ? 0.f : 1.f / L;
     const int x = x0 + row, tok = fast_quot(x, a.by_g);
     const int64_t to = (int64_t)(it.row0 + tok) * a.hq + c * g + (x - tok * g);
-    u32x2 w;
-    w[0] = pack_bf16x2(acc[0] * inv, acc[1] * inv);
-    w[1] = pack_bf16x2(acc[2] * inv, acc[3] * inv);
-    *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + to * D + e0) = w;
+    store_bf16x4(a.out, to * D + e0, acc * inv);
     if (a.lse && e0 == 0) a.lse[to] = (M + __log2f(L)) * kLn2;
   }
 }

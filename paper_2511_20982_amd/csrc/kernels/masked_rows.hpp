@@ -1,4 +1,4 @@
-// Windowed and tree attention for requests of more than 16 packed rows (chunks,
+// Windowed and tree attention for requests of more than 64 packed rows (chunks,
 // larger trees), bf16 in / fp32 accumulate, over bf16 or E4M3 pages.
 //
 // Workgroup = 4 waves = an item of 128 packed rows of one (request, KV head), 32 rows
@@ -31,13 +31,20 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
   constexpr int RS = D + 8;     // padded row of the output staging
   constexpr int kStage = 32 * RS + 8 > TE ? 32 * RS + 8 : TE;  // (a wave's output block reuses a tile buffer)
   __shared__ __attribute__((aligned(16))) uint16_t sK0[kStage], sK1[kStage], sV0[kStage], sV1[kStage];
-  // Q operands KS / 2 .. of every lane, which masked steps read from here: held in
-  // registers there too, some were spilled, and a reload waits for the tiles in flight.
+  // Q operands KS / 2 .. of every lane, read from here by every step but a tree's full
+  // ones: held in registers there too, some were spilled, and a reload waits for the
+  // tiles in flight (16 chunks of 512, window 4096, bf16: 298 us, and 264 this way).
   __shared__ __attribute__((aligned(16))) uint16_t sQ[KS / 2 * kRowsThreads * 8];
 
   ma_items<kMaMany>(a, grid_block(blockIdx.x, blockIdx.y), [&](const MaItem& it) {
-  const int tid = (int)threadIdx.x, l = lane_id();
-  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // The lane, found anew for each phase of an item, with the addresses that follow from
+  // it: held over the whole item they are spilled, and reloaded in the steps.
+  int l = lane_id(), hi = l >> 5;
+  auto renew = [&] {
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=&v"(l));
+    hi = l >> 5;
+  };
+  const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int g = (int)a.by_g.d, c = it.c, hkv = a.hkv;
   const int rows = it.n * g;               // packed rows of the request
   const int x0 = it.rt * ROWS;             // first of this item
@@ -51,13 +58,15 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
   if (v0 >= v1) return;
   const int low_key = ma_low_key(a.rule, p0);
 
-  const int hi = l >> 5;
   const int xw = x0 + 32 * w;              // first packed row of this wave
   const bool active = xw < rows;           // uniform
-  const int x = min(xw + (l & 31), rows - 1);  // (rows past the end repeat the last; not stored)
-  const int tok = fast_quot(x, a.by_g);
-  const int64_t qrow = (int64_t)(it.row0 + tok) * a.hq + c * g + (x - tok * g);
-  const uint32_t* mrow = TREE ? a.mask + (int64_t)(it.row0 + tok) * a.words : nullptr;
+  // This lane's packed row (past the end: the last, not stored), token and row of Q.
+  auto row_of = [&] { return min(xw + (l & 31), rows - 1); };
+  auto token_of = [&] { return fast_quot(row_of(), a.by_g); };
+  auto q_row = [&] {
+    const int x = row_of(), tok = fast_quot(x, a.by_g);
+    return (int64_t)(it.row0 + tok) * a.hq + c * g + (x - tok * g);
+  };
 
   // Q^T operand: Q[row][16 ks + 8 hi + 0..7] (E4M3: the dims a 16-byte read of a K
   // row gives a lane over two k-steps).  The upper half stays in LDS (this lane's own
@@ -65,15 +74,15 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
   constexpr int KH = KS / 2;
   bf16x8 qlo[KH];
   {
-    const uint16_t* qp = static_cast<const uint16_t*>(a.q) + qrow * D + (KV8 ? 16 : 8) * hi;
+    const uint16_t* qp = static_cast<const uint16_t*>(a.q) + q_row() * D + (KV8 ? 16 : 8) * hi;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       const u32x4 q = *reinterpret_cast<const u32x4*>(qp + (KV8 ? 32 * (ks / 2) + 8 * (ks % 2) : 16 * ks));
       if (ks < KH) qlo[ks] = __builtin_bit_cast(bf16x8, q);
-      else *reinterpret_cast<u32x4*>(sQ + ((ks - KH) * kRowsThreads + tid) * 8) = q;
+      else *reinterpret_cast<u32x4*>(sQ + ((ks - KH) * kRowsThreads + 64 * w + l) * 8) = q;
     }
   }
-  auto qhi_lds = [&](int i) { return *reinterpret_cast<const bf16x8*>(sQ + (i * kRowsThreads + tid) * 8); };
+  auto qhi_lds = [&](int i) { return *reinterpret_cast<const bf16x8*>(sQ + (i * kRowsThreads + 64 * w + l) * 8); };
   f32x16 oacc[ET];
 #pragma unroll
   for (int et = 0; et < ET; ++et)
@@ -92,13 +101,15 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
   auto page_of = [&](int v) {  // (a vector load, made uniform where it is used)
     return pt[seen_page(a, (KEYS / kPage) * ma_tile(kt, min(v, v1 - 1)) + w, low_key, end)];
   };
-  const int k_t = 16 * w + (l >> 2);
-  const int pk_slot = ((l >> 2) & 3) | ((l >> 3) & 4) | ((l >> 1) & 8);
-  const int lane_k = KV8 ? [&] {
-    const int s8 = l / NCH8, pc = l % NCH8;
-    return ((s8 & 3) | ((s8 & 4) << 1) | ((s8 & 8) >> 1)) * D + 16 * (pc ^ (s8 % NCH8));
-  }() : pk_slot * (2 * D) + 16 * ((l & 3) ^ ((k_t >> 2) & 3));
-  const int lane_v = KV8 ? 16 * l : (l & 31) * (2 * kPage) + 16 * (l >> 5);
+  auto lane_k = [&] {
+    if constexpr (KV8) {
+      const int s8 = l / NCH8, pc = l % NCH8;
+      return ((s8 & 3) | ((s8 & 4) << 1) | ((s8 & 8) >> 1)) * D + 16 * (pc ^ (s8 % NCH8));
+    }
+    const int k_t = 16 * w + (l >> 2), slot = ((l >> 2) & 3) | ((l >> 3) & 4) | ((l >> 1) & 8);
+    return slot * (2 * D) + 16 * ((l & 3) ^ ((k_t >> 2) & 3));
+  };
+  auto lane_v = [&] { return KV8 ? 16 * l : (l & 31) * (2 * kPage) + 16 * (l >> 5); };
   constexpr int kPageBytes = kPage * D * (KV8 ? 1 : 2);
   auto stage = [&](const void* pool, uint16_t* lds, int page, int lane_off, int step) {
     const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(
@@ -114,8 +125,6 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
   constexpr int kStepK = KV8 ? 4 * D : 64, kStepV = KV8 ? 1024 : 64 * kPage;
 
   // A operands of the QK MFMA: K[32 tt + l % 32][16 ks + 8 hi + 0..7].
-  const int kr_m = hi ^ ((l >> 2) & 3);
-  const int kr_even = (l & 31) * 32 + 8 * kr_m, kr_odd = (l & 31) * 32 + 8 * (kr_m ^ 2);
   auto kread = [&](const uint16_t* sk, int tt, bf16x8 (&ka)[KS]) {
     if constexpr (KV8) {
       const int row = 32 * tt + (l & 31);
@@ -123,10 +132,12 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
       for (int p = 0; p < KS / 2; ++p) {
         const u32x4 q = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint8_t*>(sk) + row * D +
                                                         16 * ((2 * p + hi) ^ (row % NCH8)));
-        ka[2 * p] = __builtin_bit_cast(bf16x8, few_v_operand(u32x2{q[0], q[1]}));
-        ka[2 * p + 1] = __builtin_bit_cast(bf16x8, few_v_operand(u32x2{q[2], q[3]}));
+        ka[2 * p] = v_operand(u32x2{q[0], q[1]});
+        ka[2 * p + 1] = v_operand(u32x2{q[2], q[3]});
       }
     } else {
+      const int kr_m = hi ^ ((l >> 2) & 3);
+      const int kr_even = (l & 31) * 32 + 8 * kr_m, kr_odd = (l & 31) * 32 + 8 * (kr_m ^ 2);
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks)
         ka[ks] = *reinterpret_cast<const bf16x8*>(sk + (ks >> 1) * (KEYS * 32) + tt * 1024 + ((ks & 1) ? kr_odd : kr_even));
@@ -135,8 +146,8 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
   // A operand of P.V k-step kk: V^T[32 et + l % 32][keys 16 kk + 8 hi + 0..7].
   auto vread = [&](const uint16_t* sv, int kk, int et) {
     if constexpr (KV8)
-      return few_v_operand(*reinterpret_cast<const u32x2*>(reinterpret_cast<const uint8_t*>(sv) + kk * (kPage * D) +
-                                                           (32 * et + (l & 31)) * kPage + 8 * hi));
+      return *reinterpret_cast<const u32x2*>(reinterpret_cast<const uint8_t*>(sv) + kk * (kPage * D) +
+                                             (32 * et + (l & 31)) * kPage + 8 * hi);
     else
       return *reinterpret_cast<const u32x4*>(sv + ((et * 8 + 2 * kk + hi) * 32 + (l & 31)) * 8);
   };
@@ -191,12 +202,14 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
     for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
       for (int et = 0; et < ET; ++et)
-        oacc[et] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vread(sv, kk, et)), p[kk], oacc[et], 0,
+        oacc[et] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(vread(sv, kk, et)), p[kk], oacc[et], 0,
                                                            0, 0);
   };
   // Scales the scores and makes those of what a row does not see -inf; sees: by 32
   // keys of the tile.  (Scaled here, not in the exponent, for scales of any sign.)
   auto hide = [&](f32x16 (&s)[2], int base, uint32_t (&sees)[2]) {
+    const int tok = token_of();
+    const uint32_t* mrow = TREE ? a.mask + (int64_t)(it.row0 + tok) * a.words : nullptr;
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
       sees[tt] = row_sees<TREE>(a, base + 32 * tt, pre, end, pre + tok, mrow) >> (8 * hi);
@@ -213,34 +226,42 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
     const uint32_t live = any_sees<TREE>(a, KEYS * ma_tile(kt, v) + kPage * w, p0, end) & 0xffff;  // uniform
     if (live == 0xffff) return;
     __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
-    if constexpr (KV8) {  // [D dim rows][16 key bytes]
-      u32x4 keep;
+    if constexpr (KV8) {  // [D dim rows][16 key bytes]: two halves a row
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t b = live >> (4 * i);
-        keep[i] = (b & 1 ? 0xffu : 0u) | (b & 2 ? 0xff00u : 0u) | (b & 4 ? 0xff0000u : 0u) | (b & 8 ? 0xff000000u : 0u);
-      }
-#pragma unroll
-      for (int i = 0; i < D / 64; ++i) {
-        u32x4* x = reinterpret_cast<u32x4*>(reinterpret_cast<uint8_t*>(sv) + w * (kPage * D) + (l + 64 * i) * 16);
-        *x &= keep;
+      for (int i = 0; i < D / 32; ++i) {
+        const int j = l + 64 * i;
+        u32x2* x = reinterpret_cast<u32x2*>(reinterpret_cast<uint8_t*>(sv) + w * (kPage * D) + j * 8);
+        *x = keep_of(*x, live >> (8 * (j & 1)));
       }
     } else {
 #pragma unroll
       for (int et = 0; et < ET; ++et) {
         u32x4* x = reinterpret_cast<u32x4*>(sv + ((et * 8 + 2 * w + hi) * 32 + (l & 31)) * 8);
-        *x = keep_bf16x8(*x, live >> (8 * hi));
+        *x = keep_of(*x, live >> (8 * hi));
       }
     }
   };
-  // Do all rows of the item see all of visited tile v? (uniform)
-  auto full = [&](int v) { return c_in > 0.f && all_see<TREE>(a, KEYS * ma_tile(kt, v), KEYS, pre, p0, p1); };
-  // End of the run of full tiles that v begins.
-  auto run_end = [&](int v) {
-    if constexpr (TREE) return min(v1, pre / KEYS);
+  // Does no row of this wave (positions pw0 .. pw1) see any of visited tile v?  (By wave,
+  // not by item: of the few tiles at a window's two ends a wave finds most either whole
+  // or empty.)
+  const int pw0 = pre + fast_quot(min(xw, rows - 1), a.by_g), pw1 = pre + fast_quot(min(xw + 31, rows - 1), a.by_g);
+  auto none = [&](int v) {
+    if constexpr (TREE) return false;
     const int base = KEYS * ma_tile(kt, v);
-    return min(v1, base > p1 - a.rule.window ? (p0 + 1) / KEYS - kt.low + kt.nsink : min(p0 + 1, a.rule.sinks) / KEYS);
+    return base > pw1 || (base + KEYS <= pw0 - a.rule.window + 1 && base >= a.rule.sinks);
   };
+  // The run of full tiles [va, ve) that a wave takes without masks: up to its rows'
+  // positions, behind the windows' starts.  (Full tiles of sinks go with the masked.)
+  int va = v0, ve = v0;
+  if (c_in > 0.f) {
+    if constexpr (TREE) {
+      ve = min(v1, pre / KEYS);
+    } else {
+      const int low = (max(pw1 - a.rule.window + 1, 0) + KEYS - 1) / KEYS;
+      va = min(v1, max(v0, low - kt.low + kt.nsink));
+      ve = min(v1, (pw0 + 1) / KEYS - kt.low + kt.nsink);
+    }
+  }
 
   // K tile i (of v0 + i) sits in K buffer i % 2, V tile i in V buffer i % 2, K a tile
   // ahead.  Step i loads K tile i + 2 and V tile i + 1 and, after (or while) it forms
@@ -250,8 +271,8 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
   auto kbuf = [&](int b) { return b ? sK1 : sK0; };
   auto vbuf = [&](int b) { return b ? sV1 : sV0; };
   auto prefetch = [&](int par, int v) {
-    if (v + 2 < v1) stage(a.k_pool, kbuf(par), pid_k, lane_k, kStepK);
-    if (v + 1 < v1) stage(a.v_pool, vbuf(par ^ 1), pid_v, lane_v, kStepV);
+    if (v + 2 < v1) stage(a.k_pool, kbuf(par), pid_k, lane_k(), kStepK);
+    if (v + 1 < v1) stage(a.v_pool, vbuf(par ^ 1), pid_v, lane_v(), kStepV);
     pid_v = pid_k;
     pid_k = __builtin_amdgcn_readfirstlane(ahead);  // (landed at the last barrier)
     ahead = page_of(v + 4);
@@ -259,19 +280,17 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
   {
     const int first = __builtin_amdgcn_readfirstlane(page_of(v0));
     pid_v = __builtin_amdgcn_readfirstlane(page_of(v0 + 1));
-    stage(a.k_pool, sK0, first, lane_k, kStepK);
-    if (v0 + 1 < v1) stage(a.k_pool, sK1, pid_v, lane_k, kStepK);
-    stage(a.v_pool, sV0, first, lane_v, kStepV);
+    stage(a.k_pool, sK0, first, lane_k(), kStepK);
+    if (v0 + 1 < v1) stage(a.k_pool, sK1, pid_v, lane_k(), kStepK);
+    stage(a.v_pool, sV0, first, lane_v(), kStepV);
     pid_k = __builtin_amdgcn_readfirstlane(page_of(v0 + 2));
     ahead = page_of(v0 + 3);
     clear_dead(sV0, v0);
   }
   __syncthreads();
   f32x16 sa[2], sb[2];  // S^T of two consecutive tiles
-  if (active) {
-    qk(sK0, sa, qhi_lds);
-    if (full(v0)) m_run = row_max(sa) * c_in;
-  }
+  qk(sK0, sa, qhi_lds);
+  if (va == v0 && v0 < ve) m_run = row_max(sa) * c_in;
   __syncthreads();  // (K tile 2 goes where tile 0 was)
 
   int v = v0;
@@ -290,17 +309,22 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
     __syncthreads();
     ++v;
   };
+  auto step_none = [&](auto par) {
+    prefetch(par(), v);
+    qk(kbuf(par() ^ 1), sa, qhi_lds);
+    clear_dead(vbuf(par() ^ 1), v + 1);
+    __syncthreads();
+    ++v;
+  };
   // A full tile.  No maximum is taken: the weights are formed against the running
   // one, and only a sum beyond 2^20 (a tile far above it, the first one seen) takes it.
-  bf16x8 qhi[KH];
-  auto qhi_reg = [&](int i) { return qhi[i]; };
-  auto step_full = [&](f32x16 (&sc)[2], f32x16 (&sn)[2], auto par) {
+  auto step_full = [&](f32x16 (&sc)[2], f32x16 (&sn)[2], auto par, auto qhi) {
     prefetch(par(), v);
-    qk(kbuf(par() ^ 1), sn, qhi_reg);
+    qk(kbuf(par() ^ 1), sn, qhi);
     if constexpr (!KV8) {
       // The K reads spread over the products: all of them ahead, Q operands are
       // spilled, and a reload waits for the tiles in flight.
-      constexpr int kMfma = 0x008, kDsRead = 0x100, kAhead = KS + 2;
+      constexpr int kMfma = 0x008, kDsRead = 0x100, kAhead = TREE ? KS + 2 : 6;
       __builtin_amdgcn_sched_group_barrier(kDsRead, kAhead, 0);
 #pragma unroll
       for (int i = 0; i < (2 * KS - kAhead + 1) / 2; ++i) {
@@ -330,42 +354,60 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
       __syncthreads();
     }
   }
-  while (v < v1) {
-    if (!full(v)) {
-      if ((v - v0) & 1) step_masked(odd);
-      else step_masked(even);
-      continue;
+  auto masked_until = [&](int to) {
+    while (v < to) {
+      if (none(v)) {
+        if ((v - v0) & 1) step_none(odd);
+        else step_none(even);
+      } else {
+        if ((v - v0) & 1) step_masked(odd);
+        else step_masked(even);
+      }
     }
-    const int ve = run_end(v);
-#pragma unroll
-    for (int i = 0; i < KH; ++i) qhi[i] = qhi_lds(i);
+  };
+  // Tiles v .. ve - 1, all full.
+  auto full_until_ve = [&](auto qhi) {
     if ((v - v0) & 1) {
-      step_full(sa, sb, odd);
+      step_full(sa, sb, odd, qhi);
       keep_b();
     }
     while (v + 1 < ve) {
-      step_full(sa, sb, even);
-      step_full(sb, sa, odd);
+      step_full(sa, sb, even, qhi);
+      step_full(sb, sa, odd, qhi);
     }
     if (v < ve) {
-      step_full(sa, sb, even);
+      step_full(sa, sb, even, qhi);
       keep_b();
     }
+  };
+  if constexpr (TREE) {  // (Q stays in registers for the run, which is nearly all there is)
+    while (v < v1) {
+      renew();
+      if (v < ve) {
+        bf16x8 qhi[KH];
+#pragma unroll
+        for (int i = 0; i < KH; ++i) qhi[i] = qhi_lds(i);
+        full_until_ve([&](int i) { return qhi[i]; });
+      } else if ((v - v0) & 1) {
+        step_masked(odd);
+      } else {
+        step_masked(even);
+      }
+    }
+  } else {
+    renew();
+    masked_until(va < ve ? va : v1);
+    renew();
+    if (v < ve) full_until_ve(qhi_lds);
+    renew();
+    masked_until(v1);
+    renew();
   }
 
   // A value that is not finite, in a tile that only some rows see, has reached rows
   // that do not see it (0 * inf): then the item is computed again, row by row there.
-  bool bad = false;
-  {
-    float top = 0.f;
-#pragma unroll
-    for (int et = 0; et < ET; ++et)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) top = __builtin_elementwise_maximum(top, __builtin_fabsf(oacc[et][i]));
-    bad = !(top < INFINITY);
-  }
   uint32_t* flags = reinterpret_cast<uint32_t*>(sK1 + kStage - 8);  // (behind the output staging)
-  const bool wave_bad = active && __ballot(bad) != 0;
+  const bool wave_bad = active && any_not_finite<ET>(oacc);
   if (l == 0) flags[w] = wave_bad;
   __syncthreads();
   if (flags[0] | flags[1] | flags[2] | flags[3]) {
@@ -378,8 +420,8 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
 #pragma unroll 1
     for (int v = v0; v < v1; ++v) {
       const int page = __builtin_amdgcn_readfirstlane(page_of(v));
-      stage(a.k_pool, sK0, page, lane_k, kStepK);
-      stage(a.v_pool, sV0, page, lane_v, kStepV);
+      stage(a.k_pool, sK0, page, lane_k(), kStepK);
+      stage(a.v_pool, sV0, page, lane_v(), kStepV);
       __syncthreads();
       if (active) {
         uint32_t sees[2];
@@ -396,7 +438,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
 #pragma unroll
             for (int et = 0; et < ET; ++et) {
               const f32x16 o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                  __builtin_bit_cast(bf16x8, keep_bf16x8(vread(sV0, kk, et), see)), p[kk], oacc[et], 0, 0, 0);
+                  v_operand(keep_of(vread(sV0, kk, et), see)), p[kk], oacc[et], 0, 0, 0);
               if ((l & 31) == r) oacc[et] = o;
             }
           }
@@ -449,7 +491,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
           o4, reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.out) +
                                        ((int64_t)(it.row0 + ty) * a.hq + c * g + (y - ty * g)) * D + 8 * ch));
   }
-  if (a.lse && hi == 0 && mine) a.lse[qrow] = (m_run + __log2f(L)) * kLn2;
+  if (a.lse && hi == 0 && mine) a.lse[q_row()] = (m_run + __log2f(L)) * kLn2;
   }
   }
   __syncthreads();  // (the next item's tiles)

@@ -45,21 +45,21 @@ constexpr KeyTiles ma_key_tiles(const MaskRule& m, int p0, int p1, int keys) {
 // row x is token x / g, query head c * g + x % g.  An item is (request, KV head c,
 // `rows` packed rows).
 //
-// The few-row kernel takes requests of at most kMaFewRows packed rows, the
-// many-row kernel the others; a call with both launches both.  The fp32 kernel
-// takes all of them.
-constexpr int kMaFewRows = 16;
-
-enum { kMaFew = 0, kMaMany = 1, kMaF32 = 2 };
-struct MaKind {  // of a kernel: packed rows of an item, keys of a tile
-  int which, rows, keys;
+// Kernels, by the packed rows of a request: one for up to 16, one for up to 64, a
+// many-row kernel with items of 128, the fp32 kernel for any.  A kernel of a call
+// takes the requests whose rows lie in (lo, hi].
+enum { kMaFew = 0, kMaMid = 1, kMaMany = 2, kMaF32 = 3, kMaKinds = 4 };
+struct MaKind {
+  int which, rows, keys;  // packed rows of an item, keys of a tile
+  int lo, hi;
 };
-constexpr MaKind ma_kind(int which) {
-  return which == kMaFew ? MaKind{kMaFew, kMaFewRows, 32} : which == kMaMany ? MaKind{kMaMany, 128, 64} : MaKind{kMaF32, 16, 16};
+constexpr MaKind ma_kind(int which, int lo = 0, int hi = INT32_MAX) {
+  return which == kMaFew    ? MaKind{kMaFew, 16, 32, lo, hi}
+         : which == kMaMid  ? MaKind{kMaMid, 64, 32, lo, hi}
+         : which == kMaMany ? MaKind{kMaMany, 128, 64, lo, hi}
+                            : MaKind{kMaF32, 16, 16, lo, hi};
 }
-constexpr bool ma_mine(const MaKind& k, int n, int g) {
-  return n > 0 && (k.which == kMaF32 || ((int64_t)n * g <= kMaFewRows) == (k.which == kMaFew));
-}
+constexpr bool ma_mine(const MaKind& k, int n, int g) { return n > 0 && (int64_t)n * g > k.lo && (int64_t)n * g <= k.hi; }
 constexpr int ma_row_tiles(int n, int g, int rows) { return (n * g + rows - 1) / rows; }
 
 // A bound of an item's tiles that depends on the request alone (rows at positions
@@ -106,17 +106,21 @@ constexpr bool ma_part(const MaDeal& d, int hkv, int parts, int local, int& c, i
 
 // Slices: an item is a span of `seg` units (the fixed cost of starting it) and one
 // per tile (ma_most_tiles of its request), the spans lie one after the other (by
-// request, KV head, row tile), and workgroup slice i takes the units
-// [i * total / nwg, (i + 1) * total / nwg): equal work whatever the lengths, one
-// round over the machine.  An item whose tiles lie in several slices leaves a
+// request, KV head, row tile), and every workgroup takes a slice of as many units:
+// equal work whatever the lengths, one round over the machine.  An item whose tiles lie in several slices leaves a
 // partial result in each: in slot 2 i where its part starts with the slice (or
 // earlier), else in slot 2 i + 1.  Consecutive slices run on one XCD.
-constexpr int64_t ma_slice_begin(int64_t i, int64_t total, int64_t nwg) { return i * total / nwg; }
-constexpr int64_t ma_slice_of(int64_t unit, int64_t total, int64_t nwg) {
-  int64_t i = unit * nwg / total;
-  while (i + 1 < nwg && ma_slice_begin(i + 1, total, nwg) <= unit) ++i;
-  while (i > 0 && ma_slice_begin(i, total, nwg) > unit) --i;
-  return i;
+// (32-bit arithmetic: the first total % nwg slices are a unit longer.)
+struct MaSlices {
+  int per, longer;  // units of a slice; slices of one more
+};
+constexpr MaSlices ma_slices(int64_t total, int nwg) {
+  return nwg > 0 ? MaSlices{(int)(total / nwg), (int)(total % nwg)} : MaSlices{0, 0};
+}
+constexpr int ma_slice_begin(int i, const MaSlices& s) { return i * s.per + (i < s.longer ? i : s.longer); }
+constexpr int ma_slice_of(int unit, const MaSlices& s) {
+  const int head = s.longer * (s.per + 1);
+  return unit < head ? unit / (s.per + 1) : s.longer + (unit - head) / s.per;  // (per 0: every unit is in the head)
 }
 constexpr int ma_slice_index(int b, int nwg, int xcds) {
   return nwg % xcds == 0 ? b % xcds * (nwg / xcds) + b / xcds : b;
@@ -132,7 +136,7 @@ struct MaPlan {
   int nwg;         // slices (0: whole items)
   int seg;
   int64_t total;   // units
-  bool fits;       // the counts fit the kernels' integers
+  bool fits;       // the count fits the kernels' integers
 };
 
 struct MaCosts {
@@ -178,12 +182,41 @@ inline MaPlan ma_plan(const MaskRule& m, const MaKind& k, const int32_t* cu, con
   const double whole = items <= resident ? longest : std::max(longest, work / resident + 0.5 * longest);
   const double slices = std::min(resident, std::max(1.0, bound / cost.min_tiles));
   const double sliced = (bound + slices * cost.seg) / slices + cost.merge;
-  p.fits = p.blocks <= kMaMaxUnits && p.total <= kMaMaxUnits;
-  if (k.which == kMaF32 || whole <= sliced || !p.fits) return p;
+  p.fits = p.blocks <= kMaMaxUnits;
+  if (k.which == kMaF32 || whole <= sliced || p.total > kMaMaxUnits) return p;
   p.nwg = (int)slices;
   if (p.nwg > xcds) p.nwg -= p.nwg % xcds;
   p.blocks = p.nwg;
   return p;
+}
+
+// The kernels of a call: those whose requests carry a fair share of its tiles.  A
+// class of fewer rows whose share is small goes with the next (whose kernel can take
+// it, less efficiently) rather than to a launch of its own behind the others.
+struct MaSplit {
+  int hi16, hi64;  // the first kernel takes rows up to hi16, the second up to hi64, the third the rest
+};
+inline MaSplit ma_split(const MaskRule& m, const int32_t* cu, const int32_t* pre, int nreq, int g) {
+  double tiles[3] = {0, 0, 0};  // of 32 keys
+  for (int r = 0; r < nreq; ++r) {
+    const int n = cu[r + 1] - cu[r];
+    if (n == 0) continue;
+    const int64_t rows = (int64_t)n * g;
+    const int c = rows <= 16 ? 0 : rows <= 64 ? 1 : 2;
+    tiles[c] += ma_most_tiles(m, pre[r], n, g, ma_kind(kMaMid)) * (c == 2 ? (double)ma_row_tiles(n, g, 128) : 1.);
+  }
+  constexpr double kShare = 0.25;
+  MaSplit s{16, 64};
+  if (tiles[0] < kShare * (tiles[1] + tiles[2])) {
+    s.hi16 = 0;
+    tiles[1] += tiles[0];
+  }
+  if (tiles[1] < kShare * tiles[2]) s.hi64 = s.hi16;
+  return s;
+}
+// Kernel i (0, 1, 2) of a call.
+constexpr MaKind ma_kernel(const MaSplit& s, int i) {
+  return i == 0 ? ma_kind(kMaFew, 0, s.hi16) : i == 1 ? ma_kind(kMaMid, s.hi16, s.hi64) : ma_kind(kMaMany, s.hi64);
 }
 
 // Workspace of one kernel's plan: [2 nwg][rows][D] partial outputs, then

@@ -74,7 +74,7 @@ static int check_plan(const MaskRule& m, const std::vector<int32_t>& cu, const s
   const MaDeal d = ma_deal(hkv, mach.xcds);
   MaPlan p = ma_plan(m, k, cu.data(), pre.data(), n, g, hkv, mach, cost);
   if (!p.fits) return fail("does not fit", p.blocks, p.total);
-  if (slices && p.nwg == 0 && p.blocks > 0) p.blocks = p.nwg = 1 + (int)(p.total % 97);  // (any count has to work)
+  if (slices && p.nwg == 0 && p.blocks > 0 && p.total <= kMaMaxUnits) p.blocks = p.nwg = 1 + (int)(p.total % 97);  // (any count has to work)
   struct Item {
     int r, c, rt, tiles;
     int64_t first;
@@ -107,6 +107,7 @@ static int check_plan(const MaskRule& m, const std::vector<int32_t>& cu, const s
   }
   if (units != p.total) return fail("units", units, p.total);
   if (p.nwg == 0) return base == p.blocks ? 0 : fail("blocks", base, p.blocks);
+  const MaSlices sl = ma_slices(p.total, p.nwg);
   std::set<int> order;
   for (int b = 0; b < p.nwg; ++b) order.insert(ma_slice_index(b, p.nwg, mach.xcds));
   if ((int)order.size() != p.nwg || *order.begin() != 0 || *order.rbegin() != p.nwg - 1) return fail("slice order", p.nwg, 0);
@@ -115,7 +116,7 @@ static int check_plan(const MaskRule& m, const std::vector<int32_t>& cu, const s
   std::vector<int> taken(items.size(), 0);
   size_t at = 0;
   for (int i = 0; i < p.nwg; ++i) {
-    const int64_t begin = ma_slice_begin(i, p.total, p.nwg), end = ma_slice_begin(i + 1, p.total, p.nwg);
+    const int64_t begin = ma_slice_begin(i, sl), end = ma_slice_begin(i + 1, sl);
     if (begin > end || (i == 0 && begin != 0) || (i == p.nwg - 1 && end != p.total)) return fail("slices", begin, end);
     int64_t pos = begin;
     while (at > 0 && items[at].first > pos) --at;
@@ -146,17 +147,17 @@ static int check_plan(const MaskRule& m, const std::vector<int32_t>& cu, const s
   std::set<size_t> merged;
   size_t found = 0;
   for (int slice = 1; slice < p.nwg; ++slice) {
-    const int64_t unit = ma_slice_begin(slice, p.total, p.nwg);
+    const int64_t unit = ma_slice_begin(slice, sl);
     if (unit >= p.total) continue;
     size_t i = 0;
     while (i + 1 < items.size() && items[i + 1].first <= unit) ++i;
     const Item& it = items[i];
-    const int b0 = (int)ma_slice_of(it.first + p.seg, p.total, p.nwg);
-    const int b1 = (int)ma_slice_of(it.first + p.seg + it.tiles - 1, p.total, p.nwg);
+    const int b0 = ma_slice_of((int)it.first + p.seg, sl);
+    const int b1 = ma_slice_of((int)it.first + p.seg + it.tiles - 1, sl);
     if (b0 == b1 || slice != b0 + 1) continue;
     if (!merged.insert(i).second) return fail("merged twice", i, slice);
     for (int b = b0; b <= b1; ++b) {
-      const int slot = b == b0 ? 2 * b0 + (ma_slice_begin(b0, p.total, p.nwg) >= it.first ? 0 : 1) : 2 * b;
+      const int slot = b == b0 ? 2 * b0 + (ma_slice_begin(b0, sl) >= it.first ? 0 : 1) : 2 * b;
       auto w = written.find({i, b});
       if (w == written.end() || w->second != slot) return fail("merge reads a slot that was not written", b, slot);
       ++found;
@@ -176,9 +177,9 @@ int main(int argc, char** argv) {
   for (int i = 0; i < cases; ++i) {
     const MaskRule m{pick(0, 2) == 0, log(1, 700), pick(0, 3) ? log(0, 90) : 0};
     const int g = (const int[]){1, 2, 3, 7, 8, 16, 32, 130}[pick(0, 7)];
-    for (int which : {(int)kMaFew, (int)kMaMany, (int)kMaF32}) {
-      const MaKind k = ma_kind(which);
-      const int n = which == kMaFew ? pick(1, std::max(1, 16 / g)) : log(1, 200);
+    for (int which = 0; which < kMaKinds; ++which) {
+      const MaKind k = ma_kind(which, 0, which <= kMaMid ? ma_kind(which).rows : INT32_MAX);
+      const int n = which <= kMaMid ? pick(1, std::max(1, k.rows / g)) : log(1, 200);
       if (!ma_mine(k, n, g)) continue;
       if (int rc = check_tiles(m, log(0, 900), n, g, k)) return rc;
     }
@@ -189,14 +190,25 @@ int main(int argc, char** argv) {
       pre.push_back(pick(0, 4) ? log(0, 900) : pick(0, 100000));
     }
     const MaCosts cost{pick(0, 12), pick(0, 20), pick(1, 6)};
-    for (int which : {(int)kMaFew, (int)kMaMany, (int)kMaF32})
+    const MaSplit split = ma_split(m, cu.data(), pre.data(), reqs, g);
+    std::vector<int> taken(reqs, 0);
+    for (int j = 0; j < 4; ++j) {
+      const MaKind k = j < 3 ? ma_kernel(split, j) : ma_kind(kMaF32);
+      for (int r = 0; j < 3 && r < reqs; ++r) {
+        const int len = cu[r + 1] - cu[r];
+        taken[r] += ma_mine(k, len, g);
+        if (ma_mine(k, len, g) && k.which <= kMaMid && len * g > k.rows) return fail("rows above the kernel's", len * g, k.rows);
+      }
       for (bool slices : {false, true})
-        if (int rc = check_plan(m, cu, pre, g, hkv, ma_kind(which), mach, cost, slices && which != kMaF32)) return rc;
+        if (int rc = check_plan(m, cu, pre, g, hkv, k, mach, cost, slices && j < 3)) return rc;
+    }
+    for (int r = 0; r < reqs; ++r)
+      if (taken[r] != (cu[r + 1] > cu[r])) return fail("a request is not taken once", r, taken[r]);
   }
   // Positions and windows at their limits do not overflow.
-  for (int which : {(int)kMaFew, (int)kMaMany, (int)kMaF32}) {
+  for (int which = 0; which < kMaKinds; ++which) {
     const MaKind k = ma_kind(which);
-    const int32_t cu[2] = {0, which == kMaFew ? 1 : 17}, pre[1] = {kMaMaxPos - 17};
+    const int32_t cu[2] = {0, which <= kMaMid ? 1 : 17}, pre[1] = {kMaMaxPos - 17};
     for (const MaskRule m : {MaskRule{1, 0, 0}, MaskRule{0, kMaMaxPos, kMaMaxPos}, MaskRule{0, 1, 0}}) {
       const MaPlan p = ma_plan(m, k, cu, pre, 1, 1, 8, mach, MaCosts{3, 6, 3});
       if (p.blocks < 8 || p.total < 8) return fail("largest positions", p.blocks, p.total);
