@@ -33,17 +33,11 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
   __shared__ __attribute__((aligned(16))) uint16_t sK0[kStage], sK1[kStage], sV0[kStage], sV1[kStage];
   // Q operands KS / 2 .. of every lane, read from here by every step but a tree's full
   // ones: held in registers there too, some were spilled, and a reload waits for the
-  // tiles in flight (16 chunks of 512, window 4096, bf16: 298 us, and 264 this way).
+  // tiles in flight (16 chunks of 512 x 32 heads, window 1024, bf16: 298 us, and 264 this way).
   __shared__ __attribute__((aligned(16))) uint16_t sQ[KS / 2 * kRowsThreads * 8];
 
   ma_items<kMaMany>(a, grid_block(blockIdx.x, blockIdx.y), [&](const MaItem& it) {
-  // The lane, found anew for each phase of an item, with the addresses that follow from
-  // it: held over the whole item they are spilled, and reloaded in the steps.
-  int l = lane_id(), hi = l >> 5;
-  auto renew = [&] {
-    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=&v"(l));
-    hi = l >> 5;
-  };
+  const int l = lane_id(), hi = l >> 5;
   const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int g = (int)a.by_g.d, c = it.c, hkv = a.hkv;
   const int rows = it.n * g;               // packed rows of the request
@@ -60,12 +54,29 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
 
   const int xw = x0 + 32 * w;              // first packed row of this wave
   const bool active = xw < rows;           // uniform
-  // This lane's packed row (past the end: the last, not stored), token and row of Q.
-  auto row_of = [&] { return min(xw + (l & 31), rows - 1); };
-  auto token_of = [&] { return fast_quot(row_of(), a.by_g); };
-  auto q_row = [&] {
-    const int x = row_of(), tok = fast_quot(x, a.by_g);
+  // Lane l's packed row (past the end: the last, not stored), token and row of Q.
+  auto row_of = [&](int l) { return min(xw + (l & 31), rows - 1); };
+  auto token_of = [&](int l) { return fast_quot(row_of(l), a.by_g); };
+  auto q_row = [&](int l) {
+    const int x = row_of(l), tok = fast_quot(x, a.by_g);
     return (int64_t)(it.row0 + tok) * a.hq + c * g + (x - tok * g);
+  };
+  // Scores are c_in > 0 times K . Q: the scale's sign goes to Q, and so does a scale of
+  // 0 (inf becomes NaN there, as it would).
+  const float scale = KV8 ? a.scale * a.k_scale[c] : a.scale;
+  const float c_in = scale == 0.f ? 1.f : __builtin_fabsf(scale);
+  auto signed_q = [&](u32x4 q) {
+    if (!(scale > 0.f)) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (scale < 0.f) {
+          q[i] ^= 0x80008000u;
+        } else if (scale == 0.f) {
+          const uint32_t lo = q[i] & 0x7f80, top = q[i] & 0x7f800000;
+          q[i] = (lo == 0x7f80 ? 0x7fc0u : 0u) | (top == 0x7f800000 ? 0x7fc00000u : 0u);
+        }
+    }
+    return q;
   };
 
   // Q^T operand: Q[row][16 ks + 8 hi + 0..7] (E4M3: the dims a 16-byte read of a K
@@ -74,10 +85,10 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
   constexpr int KH = KS / 2;
   bf16x8 qlo[KH];
   {
-    const uint16_t* qp = static_cast<const uint16_t*>(a.q) + q_row() * D + (KV8 ? 16 : 8) * hi;
+    const uint16_t* qp = static_cast<const uint16_t*>(a.q) + q_row(l) * D + (KV8 ? 16 : 8) * hi;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
-      const u32x4 q = *reinterpret_cast<const u32x4*>(qp + (KV8 ? 32 * (ks / 2) + 8 * (ks % 2) : 16 * ks));
+      const u32x4 q = signed_q(*reinterpret_cast<const u32x4*>(qp + (KV8 ? 32 * (ks / 2) + 8 * (ks % 2) : 16 * ks)));
       if (ks < KH) qlo[ks] = __builtin_bit_cast(bf16x8, q);
       else *reinterpret_cast<u32x4*>(sQ + ((ks - KH) * kRowsThreads + 64 * w + l) * 8) = q;
     }
@@ -89,7 +100,6 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
 #pragma unroll
     for (int i = 0; i < 16; ++i) oacc[et][i] = 0.f;
   float m_run = -INFINITY, l_run = 0.f;
-  const float c_in = KV8 ? a.scale * a.k_scale[c] : a.scale;
 
   // ---- tiles: wave w brings page w of a tile.  K (bf16) in 16-byte chunks,
   // [D / 32 chunk groups][64 rows][4 slots], chunk ch of row t in slot (ch % 4) ^
@@ -205,17 +215,19 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
         oacc[et] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(vread(sv, kk, et)), p[kk], oacc[et], 0,
                                                            0, 0);
   };
-  // Scales the scores and makes those of what a row does not see -inf; sees: by 32
-  // keys of the tile.  (Scaled here, not in the exponent, for scales of any sign.)
+  // Makes the scores of what a row does not see -inf; sees: by 32 keys of the tile.  The
+  // lane is found anew, so that nothing for it is held (and spilled) over other steps.
   auto hide = [&](f32x16 (&s)[2], int base, uint32_t (&sees)[2]) {
-    const int tok = token_of();
+    int l;
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=&v"(l));
+    const int tok = token_of(l);
     const uint32_t* mrow = TREE ? a.mask + (int64_t)(it.row0 + tok) * a.words : nullptr;
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
-      sees[tt] = row_sees<TREE>(a, base + 32 * tt, pre, end, pre + tok, mrow) >> (8 * hi);
+      sees[tt] = row_sees<TREE>(a, base + 32 * tt, pre, end, pre + tok, mrow) >> (8 * (l >> 5));
 #pragma unroll
       for (int i = 0; i < 16; ++i)  // accumulator row i is key 16 (i / 8) + 8 hi + i % 8
-        s[tt][i] = sees[tt] >> (16 * (i >> 3) + (i & 7)) & 1 ? s[tt][i] * c_in : -INFINITY;
+        s[tt][i] = sees[tt] >> (16 * (i >> 3) + (i & 7)) & 1 ? s[tt][i] : -INFINITY;
     }
   };
   // V of positions of visited tile v that no row of the item sees (slots that may hold
@@ -241,26 +253,25 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
       }
     }
   };
-  // Does no row of this wave (positions pw0 .. pw1) see any of visited tile v?  (By wave,
-  // not by item: of the few tiles at a window's two ends a wave finds most either whole
-  // or empty.)
+  // What this wave (positions pw0 .. pw1) has to do, by wave and not by item, because of
+  // the few tiles at a window's two ends a wave finds most either whole or empty: tiles
+  // va .. ve - 1 are seen in full by its rows (full tiles of sinks go with the masked),
+  // none from vl on.
   const int pw0 = pre + fast_quot(min(xw, rows - 1), a.by_g), pw1 = pre + fast_quot(min(xw + 31, rows - 1), a.by_g);
   auto none = [&](int v) {
     if constexpr (TREE) return false;
     const int base = KEYS * ma_tile(kt, v);
-    return base > pw1 || (base + KEYS <= pw0 - a.rule.window + 1 && base >= a.rule.sinks);
+    return base + KEYS <= pw0 - a.rule.window + 1 && base >= a.rule.sinks;
   };
-  // The run of full tiles [va, ve) that a wave takes without masks: up to its rows'
-  // positions, behind the windows' starts.  (Full tiles of sinks go with the masked.)
-  int va = v0, ve = v0;
-  if (c_in > 0.f) {
-    if constexpr (TREE) {
-      ve = min(v1, pre / KEYS);
-    } else {
-      const int low = (max(pw1 - a.rule.window + 1, 0) + KEYS - 1) / KEYS;
-      va = min(v1, max(v0, low - kt.low + kt.nsink));
-      ve = min(v1, (pw0 + 1) / KEYS - kt.low + kt.nsink);
-    }
+  int va = v0, ve, vl;
+  if constexpr (TREE) {
+    ve = min(v1, pre / KEYS);
+    vl = active ? v1 : v0;
+  } else {
+    const int low = (max(pw1 - a.rule.window + 1, 0) + KEYS - 1) / KEYS;
+    va = max(v0, low - kt.low + kt.nsink);
+    ve = min(v1, (pw0 + 1) / KEYS - kt.low + kt.nsink);
+    vl = active ? min(v1, max(v0, pw1 / KEYS + 1 - kt.low + kt.nsink)) : v0;
   }
 
   // K tile i (of v0 + i) sits in K buffer i % 2, V tile i in V buffer i % 2, K a tile
@@ -293,115 +304,55 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
   if (va == v0 && v0 < ve) m_run = row_max(sa) * c_in;
   __syncthreads();  // (K tile 2 goes where tile 0 was)
 
+  // A tile's maximum is taken where it is masked.  A full one's weights are formed
+  // against the running maximum, and only a sum beyond 2^20 (a tile far above it, the
+  // first one seen) takes it.
   int v = v0;
-  auto even = [] { return 0; };
-  auto odd = [] { return 1; };
-  // A tile that some row does not see in full.
-  auto step_masked = [&](auto par) {
+  auto step = [&](f32x16 (&sc)[2], f32x16 (&sn)[2], auto par) {
     prefetch(par(), v);
-    uint32_t sees[2];
-    hide(sa, KEYS * ma_tile(kt, v), sees);
-    rescale(fmaxf(m_run, row_max(sa)));
-    l_run += weights(sa, 1.f, m_run == -INFINITY ? 0.f : m_run);  // (nothing seen so far: weights 0)
-    pv(vbuf(par()));
-    qk(kbuf(par() ^ 1), sa, qhi_lds);
-    clear_dead(vbuf(par() ^ 1), v + 1);
-    __syncthreads();
-    ++v;
-  };
-  auto step_none = [&](auto par) {
-    prefetch(par(), v);
-    qk(kbuf(par() ^ 1), sa, qhi_lds);
-    clear_dead(vbuf(par() ^ 1), v + 1);
-    __syncthreads();
-    ++v;
-  };
-  // A full tile.  No maximum is taken: the weights are formed against the running
-  // one, and only a sum beyond 2^20 (a tile far above it, the first one seen) takes it.
-  auto step_full = [&](f32x16 (&sc)[2], f32x16 (&sn)[2], auto par, auto qhi) {
-    prefetch(par(), v);
-    qk(kbuf(par() ^ 1), sn, qhi);
-    if constexpr (!KV8) {
-      // The K reads spread over the products: all of them ahead, Q operands are
-      // spilled, and a reload waits for the tiles in flight.
-      constexpr int kMfma = 0x008, kDsRead = 0x100, kAhead = TREE ? KS + 2 : 6;
-      __builtin_amdgcn_sched_group_barrier(kDsRead, kAhead, 0);
-#pragma unroll
-      for (int i = 0; i < (2 * KS - kAhead + 1) / 2; ++i) {
-        __builtin_amdgcn_sched_group_barrier(kMfma, 2, 0);
-        __builtin_amdgcn_sched_group_barrier(kDsRead, 2, 0);
+    if (none(v)) {
+      qk(kbuf(par() ^ 1), sn, qhi_lds);
+    } else {
+      float m_use = m_run;
+      if (v < va || v >= ve) {
+        uint32_t sees[2];
+        hide(sc, KEYS * ma_tile(kt, v), sees);
+        rescale(fmaxf(m_run, row_max(sc) * c_in));
+        m_use = m_run == -INFINITY ? 0.f : m_run;  // (nothing seen so far: weights 0)
       }
+      qk(kbuf(par() ^ 1), sn, qhi_lds);
+      if constexpr (!KV8) {
+        // The K reads spread over the products: all of them ahead, Q operands are
+        // spilled, and a reload waits for the tiles in flight.
+        constexpr int kMfma = 0x008, kDsRead = 0x100, kAhead = 6;
+        __builtin_amdgcn_sched_group_barrier(kDsRead, kAhead, 0);
+#pragma unroll
+        for (int i = 0; i < (2 * KS - kAhead + 1) / 2; ++i) {
+          __builtin_amdgcn_sched_group_barrier(kMfma, 2, 0);
+          __builtin_amdgcn_sched_group_barrier(kDsRead, 2, 0);
+        }
+      }
+      float sum = weights(sc, c_in, m_use);
+      if (__ballot(!(sum <= 1048576.f))) {
+        rescale(fmaxf(m_run, row_max(sc) * c_in));
+        sum = weights(sc, c_in, m_run == -INFINITY ? 0.f : m_run);
+      }
+      l_run += sum;
+      pv(vbuf(par()));
     }
-    float sum = weights(sc, c_in, m_run);
-    if (__ballot(!(sum <= 1048576.f))) {
-      rescale(fmaxf(m_run, row_max(sc) * c_in));
-      sum = weights(sc, c_in, m_run);
-    }
-    l_run += sum;
-    pv(vbuf(par()));
     clear_dead(vbuf(par() ^ 1), v + 1);
     __syncthreads();
     ++v;
   };
-  auto keep_b = [&] {
-#pragma unroll
-    for (int tt = 0; tt < 2; ++tt) sa[tt] = sb[tt];
-  };
-  if (!active) {  // (brings its pages; with the others' code, S^T would be live where it is not)
-    for (; v < v1; ++v) {
-      prefetch((v - v0) & 1, v);
-      clear_dead(vbuf((v - v0 + 1) & 1), v + 1);
-      __syncthreads();
-    }
+  while (v < vl) {
+    step(sa, sb, [] { return 0; });
+    if (v >= vl) break;
+    step(sb, sa, [] { return 1; });
   }
-  auto masked_until = [&](int to) {
-    while (v < to) {
-      if (none(v)) {
-        if ((v - v0) & 1) step_none(odd);
-        else step_none(even);
-      } else {
-        if ((v - v0) & 1) step_masked(odd);
-        else step_masked(even);
-      }
-    }
-  };
-  // Tiles v .. ve - 1, all full.
-  auto full_until_ve = [&](auto qhi) {
-    if ((v - v0) & 1) {
-      step_full(sa, sb, odd, qhi);
-      keep_b();
-    }
-    while (v + 1 < ve) {
-      step_full(sa, sb, even, qhi);
-      step_full(sb, sa, odd, qhi);
-    }
-    if (v < ve) {
-      step_full(sa, sb, even, qhi);
-      keep_b();
-    }
-  };
-  if constexpr (TREE) {  // (Q stays in registers for the run, which is nearly all there is)
-    while (v < v1) {
-      renew();
-      if (v < ve) {
-        bf16x8 qhi[KH];
-#pragma unroll
-        for (int i = 0; i < KH; ++i) qhi[i] = qhi_lds(i);
-        full_until_ve([&](int i) { return qhi[i]; });
-      } else if ((v - v0) & 1) {
-        step_masked(odd);
-      } else {
-        step_masked(even);
-      }
-    }
-  } else {
-    renew();
-    masked_until(va < ve ? va : v1);
-    renew();
-    if (v < ve) full_until_ve(qhi_lds);
-    renew();
-    masked_until(v1);
-    renew();
+  for (; v < v1; ++v) {  // (the others' tiles: brings its pages)
+    prefetch((v - v0) & 1, v);
+    clear_dead(vbuf((v - v0 + 1) & 1), v + 1);
+    __syncthreads();
   }
 
   // A value that is not finite, in a tile that only some rows see, has reached rows
@@ -427,8 +378,8 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
         uint32_t sees[2];
         qk(sK0, sa, qhi_lds);
         hide(sa, KEYS * ma_tile(kt, v), sees);
-        rescale(fmaxf(m_run, row_max(sa)));
-        l_run += weights(sa, 1.f, m_run == -INFINITY ? 0.f : m_run);
+        rescale(fmaxf(m_run, row_max(sa) * c_in));
+        l_run += weights(sa, c_in, m_run == -INFINITY ? 0.f : m_run);
 #pragma unroll 1
         for (int r = 0; r < 32; ++r)  // row r alone, V cleared where it sees nothing
 #pragma unroll
@@ -491,7 +442,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
           o4, reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.out) +
                                        ((int64_t)(it.row0 + ty) * a.hq + c * g + (y - ty * g)) * D + 8 * ch));
   }
-  if (a.lse && hi == 0 && mine) a.lse[q_row()] = (m_run + __log2f(L)) * kLn2;
+  if (a.lse && hi == 0 && mine) a.lse[q_row(l)] = (m_run + __log2f(L)) * kLn2;
   }
   }
   __syncthreads();  // (the next item's tiles)
