@@ -56,7 +56,7 @@ struct MaKind {
 constexpr MaKind ma_kind(int which, int lo = 0, int hi = INT32_MAX) {
   return which == kMaFew    ? MaKind{kMaFew, 16, 32, lo, hi}
          : which == kMaMid  ? MaKind{kMaMid, 64, 32, lo, hi}
-         : which == kMaMany ? MaKind{kMaMany, 128, 64, lo, hi}
+         : which == kMaMany ? MaKind{kMaMany, 128, 32, lo, hi}
                             : MaKind{kMaF32, 16, 16, lo, hi};
 }
 constexpr bool ma_mine(const MaKind& k, int n, int g) { return n > 0 && (int64_t)n * g > k.lo && (int64_t)n * g <= k.hi; }
