@@ -35,9 +35,9 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
   constexpr int KS = D / 16;    // k-steps of the QK MFMA
   constexpr int ET = D / 32;    // O^T tiles of 32 dims
   constexpr int TE = rows_tile_elems<D, KV8>();
-  // Stage i: V of the tiles i, i + 5, .. and, one ahead, K of i + 1, i + 6, ..: what one
-  // step reads, and the next but three loads.  (Arrays of their own, so that the compiler
-  // sees that a read does not wait for the loads of other stages.)
+  // Stage i: what step i, i + 5, .. reads, K of the tile behind and V of the one before.
+  // (Arrays of their own, so that the compiler sees that a read does not wait for the
+  // loads of other stages.)
   __shared__ __attribute__((aligned(16))) uint16_t st0[2 * TE], st1[2 * TE], st2[2 * TE], st3[2 * TE], st4[2 * TE];
   static_assert(2 * TE >= 32 * D);  // (a stage takes a wave's output)
 
@@ -220,22 +220,41 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[ks], qreg[ks], s, 0, 0, 0);
   };
-  auto pv = [&](const VT (&v)[ET][2]) {
+  auto pv = [&](const uint16_t* sv) {
+    VT v[ET][2];
+#pragma unroll
+    for (int et = 0; et < ET; ++et) vread(sv, et, v[et]);
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
       for (int et = 0; et < ET; ++et)
         oacc[et] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(v[et][kk]), p[kk], oacc[et], 0, 0, 0);
   };
+  // What this wave (positions pw0 .. pw1) has to do, by wave and not by item, because of
+  // the few tiles at a window's two ends a wave finds most either whole or empty: tiles
+  // va .. ve - 1 are seen in full by its rows (full tiles of sinks go with the masked),
+  // none from vl on.
+  const int pw0 = pre + fast_quot(min(xw, rows - 1), a.by_g), pw1 = pre + fast_quot(min(xw + 31, rows - 1), a.by_g);
+  int va = v0, ve, vl;
+  if constexpr (TREE) {
+    ve = min(v1, pre / KEYS);
+    vl = active ? v1 : v0 - 1;
+  } else {
+    const int low = (max(pw1 - a.rule.window + 1, 0) + KEYS - 1) / KEYS;
+    va = max(v0, low - kt.low + kt.nsink);
+    ve = min(v1, (pw0 + 1) / KEYS - kt.low + kt.nsink);
+    vl = active ? min(v1, max(v0, pw1 / KEYS + 1 - kt.low + kt.nsink)) : v0 - 1;
+  }
+
   // Makes the scores of what a row does not see -inf; returns which of its 16 keys of
   // the tile it sees.  The lane is found anew, so that nothing for it is held (and
   // spilled) over other steps.
-  auto hide = [&](f32x16& s, int base) {
+  auto hide = [&](f32x16& s, int v) {
     int l;
     asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=&v"(l));
     const int tok = token_of(l);
     const uint32_t* mrow = TREE ? a.mask + (int64_t)(it.row0 + tok) * a.words : nullptr;
-    const uint32_t sees = row_sees<TREE>(a, base, pre, end, pre + tok, mrow) >> (16 * (l >> 5));
+    const uint32_t sees = v < vl ? row_sees<TREE>(a, KEYS * ma_tile(kt, v), pre, end, pre + tok, mrow) >> (16 * (l >> 5)) : 0;
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = sees >> i & 1 ? s[i] : -INFINITY;
     return sees;
@@ -244,7 +263,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
   // anything: 0 * NaN is NaN) is cleared in LDS by the wave that brought it, once it has
   // landed and before the barrier that publishes it.
   auto clear_dead = [&](uint16_t* sv, int v) {
-    if (v >= v1 || (kByPool && w < 2)) return;
+    if (v < v0 || v >= v1 || (kByPool && w < 2)) return;
     const uint32_t live = any_sees<TREE>(a, KEYS * ma_tile(kt, v) + kPage * wp, p0, end) & 0xffff;  // uniform
     if (live == 0xffff) return;
 #pragma unroll
@@ -259,43 +278,26 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
       }
     }
   };
-  // What this wave (positions pw0 .. pw1) has to do, by wave and not by item, because of
-  // the few tiles at a window's two ends a wave finds most either whole or empty: tiles
-  // va .. ve - 1 are seen in full by its rows (full tiles of sinks go with the masked),
-  // none from vl on.
-  const int pw0 = pre + fast_quot(min(xw, rows - 1), a.by_g), pw1 = pre + fast_quot(min(xw + 31, rows - 1), a.by_g);
-  auto none = [&](int v) {
-    if constexpr (TREE) return false;
-    const int base = KEYS * ma_tile(kt, v);
-    return base + KEYS <= pw0 - a.rule.window + 1 && base >= a.rule.sinks;
-  };
-  int va = v0, ve, vl;
-  if constexpr (TREE) {
-    ve = min(v1, pre / KEYS);
-    vl = active ? v1 : v0;
-  } else {
-    const int low = (max(pw1 - a.rule.window + 1, 0) + KEYS - 1) / KEYS;
-    va = max(v0, low - kt.low + kt.nsink);
-    ve = min(v1, (pw0 + 1) / KEYS - kt.low + kt.nsink);
-    vl = active ? min(v1, max(v0, pw1 / KEYS + 1 - kt.low + kt.nsink)) : v0;
-  }
-
-  // Step i (of tile v0 + i) loads K of tile i + 5 and V of tile i + 4 into the stage that
-  // step i - 1 read, and computes S^T of tile i + 1 while it forms the weights of tile i.
+  // Step i (of tile v0 + i) loads K of tile i + 5 and V of tile i + 3 into the stage that
+  // step i - 1 read, and does three things that do not wait for each other: S^T of tile
+  // i + 1, the weights of tile i, and the product of the weights of tile i - 1 with V.
   // It ends when what step i + 1 reads has landed: this wave's loads of the three steps
   // before may be in flight then.
-  int pid_k = page_of(v0), pid_v = pid_k;
+  int pid_k = page_of(v0), pid_k1 = pid_k, pid_v = pid_k;
   auto issue = [&](int v, uint16_t* st) {
     const int next = page_of(v + 6);
-    load(st, pid_k, v + 5 < v1, pid_v, v + 4 >= v0 && v + 4 < v1);
-    pid_v = pid_k;
+    load(st, pid_k, v + 5 < v1, pid_v, v + 3 >= v0 && v + 3 < v1);
+    pid_v = pid_k1;
+    pid_k1 = pid_k;
     pid_k = next;
   };
   auto finish = [&](int v, uint16_t* next) {
     wait_loads<3 * kPerStep>();
-    clear_dead(next + TE, v + 1);
+    clear_dead(next + TE, v);
     lds_barrier();
   };
+  for (int i = (int)threadIdx.x; i < TE / 8; i += kRowsThreads)  // (step 0: weights 0 and no V)
+    reinterpret_cast<u32x4*>(st0 + TE)[i] = u32x4{0, 0, 0, 0};
   issue(v0 - 5, st4);
   issue(v0 - 4, st0);
   issue(v0 - 3, st1);
@@ -304,56 +306,40 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
   finish(v0 - 1, st0);
   f32x16 sa, sb;  // S^T of two consecutive tiles
   qk(st4, sa);
-  if (va == v0 && v0 < ve) m_run = row_max(sa) * c_in;
   lds_barrier();  // (step 0 loads into st4)
 
-  // A tile's maximum is taken where it is masked.  A full one's weights are formed
-  // against the running maximum, and only a sum beyond 2^20 (a tile far above it, the
-  // first one seen) takes it.
+  // Weights are formed against the running maximum, and only a sum beyond 2^20 (a tile
+  // far above it, the first one seen: NaN) takes the tile's own.
   int v = v0;
+  p[0] = p[1] = bf16x8{};
   auto step = [&](f32x16& sc, f32x16& sn, uint16_t* before, const uint16_t* now, uint16_t* next) {
     issue(v, before);
-    if (none(v)) {
-      qk(now, sn);
-    } else {
-      float m_use = m_run;
-      if (v < va || v >= ve) {
-        hide(sc, KEYS * ma_tile(kt, v));
-        rescale(fmaxf(m_run, row_max(sc) * c_in));
-        m_use = m_run == -INFINITY ? 0.f : m_run;  // (nothing seen so far: weights 0)
-      }
-      qk(now, sn);
-      // V is read ahead of the weights, and held here: read where the products need it,
-      // each of them waits for its operand.
-      VT vv[ET][2];
-#pragma unroll
-      for (int et = 0; et < ET; ++et) vread(now + TE, et, vv[et]);
-      float sum = weights(sc, c_in, m_use);
-#pragma unroll
-      for (int et = 0; et < ET; ++et) asm volatile("" : "+v"(vv[et][0]), "+v"(vv[et][1]), "+v"(sum));
-      if (__ballot(!(sum <= 1048576.f))) {
-        rescale(fmaxf(m_run, row_max(sc) * c_in));
-        sum = weights(sc, c_in, m_run == -INFINITY ? 0.f : m_run);
-      }
-      l_run += sum;
-      pv(vv);
+    if (v < va || v >= ve) hide(sc, v);
+    qk(now, sn);
+    pv(now + TE);
+    float sum = weights(sc, c_in, m_run);
+    if (__ballot(!(sum <= 1048576.f))) {
+      rescale(fmaxf(m_run, row_max(sc) * c_in));
+      sum = weights(sc, c_in, m_run == -INFINITY ? 0.f : m_run);  // (nothing seen so far: weights 0)
     }
+    l_run += sum;
     finish(v, next);
     ++v;
   };
-  while (v < vl) {
+  while (v <= vl) {
     step(sa, sb, st4, st0, st1);
-    if (v >= vl) break;
+    if (v > vl) break;
     step(sb, sa, st0, st1, st2);
-    if (v >= vl) break;
+    if (v > vl) break;
     step(sa, sb, st1, st2, st3);
-    if (v >= vl) break;
+    if (v > vl) break;
     step(sb, sa, st2, st3, st4);
-    if (v >= vl) break;
+    if (v > vl) break;
     step(sa, sb, st3, st4, st0);
     sa = sb;
   }
-  for (int i = (v - v0) % 5; v < v1; ++v) {  // (the others' tiles: brings its part)
+  int i = (v - v0) % 5;
+  for (; v <= v1; ++v) {  // (the others' tiles: brings its part)
     issue(v, i == 0 ? st4 : i == 1 ? st0 : i == 2 ? st1 : i == 3 ? st2 : st3);
     finish(v, i == 0 ? st1 : i == 1 ? st2 : i == 2 ? st3 : i == 3 ? st4 : st0);
     i = i == 4 ? 0 : i + 1;
@@ -382,7 +368,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
       __syncthreads();
       if (active) {
         qk(st0, sa);
-        const uint32_t sees = hide(sa, KEYS * ma_tile(kt, v));
+        const uint32_t sees = hide(sa, v);
         rescale(fmaxf(m_run, row_max(sa) * c_in));
         l_run += weights(sa, c_in, m_run == -INFINITY ? 0.f : m_run);
         VT vv[ET][2];
