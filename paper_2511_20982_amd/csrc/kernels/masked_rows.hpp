@@ -152,49 +152,44 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
     }
   };
 
-  // A operands of the QK MFMA: K[key of row l % 32][16 ks + 8 hi + 0..7].
-  auto kread = [&](const uint16_t* sk, bf16x8 (&ka)[KS]) {
-    const int r = 4 * ((l >> 3) & 3) + (l & 3), page = (l >> 2) & 1, sw = swizzle(r, page);
-    if constexpr (KV8) {
-      const uint8_t* row = reinterpret_cast<const uint8_t*>(sk) + (16 * page + r) * D;
-#pragma unroll
-      for (int p = 0; p < KS / 2; ++p) {
-        const u32x4 q = *reinterpret_cast<const u32x4*>(row + 16 * ((2 * p + hi) ^ sw));
-        ka[2 * p] = v_operand(u32x2{q[0], q[1]});
-        ka[2 * p + 1] = v_operand(u32x2{q[2], q[3]});
-      }
-    } else {
-      const int even = (16 * page + r) * 32 + 8 * (hi ^ sw), odd = even ^ 16;
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks)
-        ka[ks] = *reinterpret_cast<const bf16x8*>(sk + (ks >> 1) * (KEYS * 32) + ((ks & 1) ? odd : even));
-    }
+  // A operands of the QK MFMA, K[key of row l % 32][16 ks + 8 hi + 0..7], k-step by
+  // k-step (E4M3: two to a read) ..
+  const int kr = 4 * ((l >> 3) & 3) + (l & 3), kr_page = (l >> 2) & 1, kr_sw = swizzle(kr, kr_page);
+  auto read_k = [&](const uint16_t* st, int i) {
+    if constexpr (KV8)
+      return *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint8_t*>(st) + (16 * kr_page + kr) * D +
+                                             16 * ((2 * i + hi) ^ kr_sw));
+    else
+      return *reinterpret_cast<const u32x4*>(st + (i >> 1) * (KEYS * 32) + (16 * kr_page + kr) * 32 +
+                                             ((8 * (hi ^ kr_sw)) ^ (16 * (i & 1))));
   };
-  // A operands of the P.V MFMA: V^T[32 et + l % 32][keys 16 hi + 8 kk + 0..7].
-  using VT = std::conditional_t<KV8, u32x2, u32x4>;
-  auto vread = [&](const uint16_t* sv, int et, VT (&v)[2]) {
-    if constexpr (KV8) {
-      const u32x4 x = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint8_t*>(sv) + (hi * D + 32 * et + (l & 31)) * kPage);
-      v[0] = u32x2{x[0], x[1]};
-      v[1] = u32x2{x[2], x[3]};
-    } else {
-#pragma unroll
-      for (int kk = 0; kk < 2; ++kk)
-        v[kk] = *reinterpret_cast<const u32x4*>(sv + ((et * 4 + 2 * hi + kk) * 32 + (l & 31)) * 8);
-    }
+  // .. and of the P.V MFMA, V^T[32 et + l % 32][keys 16 hi + 8 kk + 0..7]: et = i % ET,
+  // kk = i / ET (E4M3: et = i, both kk).
+  auto read_v = [&](const uint16_t* st, int i) {
+    if constexpr (KV8)
+      return *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint8_t*>(st + TE) + (hi * D + 32 * i + (l & 31)) * kPage);
+    else
+      return *reinterpret_cast<const u32x4*>(st + TE + (((i % ET) * 4 + 2 * hi + i / ET) * 32 + (l & 31)) * 8);
+  };
+  constexpr int PER = KV8 ? 2 : 1;  // operands of a read
+  using Half = std::conditional_t<KV8, u32x2, u32x4>;
+  auto half_of = [&](u32x4 x, int h) {
+    if constexpr (KV8) return h ? u32x2{x[2], x[3]} : u32x2{x[0], x[1]};
+    else return x;
   };
 
   bf16x8 p[2];  // P^T: B operands of the two P.V k-steps
-  // Weights 2^(c s - m_use); returns this lane's half of the row sum.
+  float sum[4];
+  auto weight = [&](const f32x16& s, int i, float c, float m_use, bf16x8 (&p)[2]) {  // 2^(c s - m_use)
+    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, -m_use));
+    sum[i & 3] = i < 4 ? e : sum[i & 3] + e;
+    p[i >> 3][i & 7] = (__bf16)e;
+  };
+  auto total = [&] { return (sum[0] + sum[1]) + (sum[2] + sum[3]); };  // this lane's half of the row sum
   auto weights = [&](const f32x16& s, float c, float m_use) {
-    float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, -m_use));
-      sum[i & 3] += e;
-      p[i >> 3][i & 7] = (__bf16)e;
-    }
-    return (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    for (int i = 0; i < 16; ++i) weight(s, i, c, m_use, p);
+    return total();
   };
   auto row_max = [&](const f32x16& s) {
     float mx = s[0];
@@ -211,24 +206,12 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
 #pragma unroll
     for (int et = 0; et < ET; ++et) oacc[et] *= alpha;
   };
-  // S^T of a tile.
-  auto qk = [&](const uint16_t* sk, f32x16& s) {
-    bf16x8 ka[KS];
-    kread(sk, ka);
+  auto qk = [&](const uint16_t* st, f32x16& s) {  // S^T of a tile
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[ks], qreg[ks], s, 0, 0, 0);
-  };
-  auto pv = [&](const uint16_t* sv) {
-    VT v[ET][2];
-#pragma unroll
-    for (int et = 0; et < ET; ++et) vread(sv, et, v[et]);
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-      for (int et = 0; et < ET; ++et)
-        oacc[et] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(v[et][kk]), p[kk], oacc[et], 0, 0, 0);
+    for (int ks = 0; ks < KS; ++ks)
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(half_of(read_k(st, ks / PER), ks % PER)), qreg[ks], s, 0, 0, 0);
   };
   // What this wave (positions pw0 .. pw1) has to do, by wave and not by item, because of
   // the few tiles at a window's two ends a wave finds most either whole or empty: tiles
@@ -315,9 +298,35 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
   auto step = [&](f32x16& sc, f32x16& sn, uint16_t* before, const uint16_t* now, uint16_t* next) {
     issue(v, before);
     if (v < va || v >= ve) hide(sc, v);
-    qk(now, sn);
-    pv(now + TE);
-    float sum = weights(sc, c_in, m_run);
+    // The matrix products of S^T and O^T in turn, so that none waits for the one before,
+    // and between two of them what the compiler would otherwise put in front or behind:
+    // the conversion of the next operand, a read of one further on, weights.
+    constexpr int NM = KS + 2 * ET, NR = NM / PER, AHEAD = KV8 ? NR : 6;
+    u32x4 raw[NR];
+    auto read = [&](int i) { raw[i] = i % 2 == 0 ? read_k(now, i / 2) : read_v(now, i / 2); };
+    auto operand = [&](int i) {  // of product i
+      return v_operand(half_of(raw[2 * (i / (2 * PER)) + i % 2], (i / 2) % PER));
+    };
+    bf16x8 p_now[2];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) read(i);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sn[i] = 0.f;
+    bf16x8 op = operand(0);
+#pragma unroll
+    for (int i = 0; i < NM; ++i) {
+      const int j = i / 2, et = KV8 ? j / 2 : j % ET, kk = KV8 ? j % 2 : j / ET;
+      if (i + AHEAD < NR) read(i + AHEAD);
+      if (i % 2 == 0) sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op, qreg[j], sn, 0, 0, 0);
+      else oacc[et] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op, p[kk], oacc[et], 0, 0, 0);
+      if (i + 1 < NM) op = operand(i + 1);
+#pragma unroll
+      for (int e = 16 * i / NM; e < 16 * (i + 1) / NM; ++e) weight(sc, e, c_in, m_run, p_now);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    float sum = total();
+    p[0] = p_now[0];
+    p[1] = p_now[1];
     if (__ballot(!(sum <= 1048576.f))) {
       rescale(fmaxf(m_run, row_max(sc) * c_in));
       sum = weights(sc, c_in, m_run == -INFINITY ? 0.f : m_run);  // (nothing seen so far: weights 0)
@@ -371,9 +380,6 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
         const uint32_t sees = hide(sa, v);
         rescale(fmaxf(m_run, row_max(sa) * c_in));
         l_run += weights(sa, c_in, m_run == -INFINITY ? 0.f : m_run);
-        VT vv[ET][2];
-#pragma unroll
-        for (int et = 0; et < ET; ++et) vread(st0 + TE, et, vv[et]);
 #pragma unroll 1
         for (int r = 0; r < 32; ++r)  // row r alone, V cleared where it sees nothing
 #pragma unroll
@@ -381,8 +387,8 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
             const uint32_t see = (uint32_t)__shfl((int)sees, (l & 32) + r, 64) >> (8 * kk);
 #pragma unroll
             for (int et = 0; et < ET; ++et) {
-              const f32x16 o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(keep_of(vv[et][kk], see)), p[kk], oacc[et],
-                                                                       0, 0, 0);
+              const Half x = half_of(read_v(st0, KV8 ? et : kk * ET + et), kk);
+              const f32x16 o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(keep_of(x, see)), p[kk], oacc[et], 0, 0, 0);
               if ((l & 31) == r) oacc[et] = o;
             }
           }
