@@ -72,7 +72,7 @@ size_t masked_workspace_size(const dopd_attn_shape* s, const dopd::MaskRule& rul
 
 template <int D, bool KV8, bool TREE>
 dopd_status launch_masked(const dopd::MaKind& k, const dopd::MaskedArgs& a, const dopd::MaPlan& p, hipStream_t strm) {
-  const dim3 grid = grid_of(p.blocks), block(256), merge((unsigned)((p.nwg - 1) * (k.rows / dopd::merge_rows<D>())));
+  const dim3 grid = grid_of(p.blocks), block(256), merge((unsigned)((p.nwg - 1) * (k.rows / dopd::merge_rows(k.which))));
   switch (k.which) {
     case dopd::kMaFew: hipLaunchKernelGGL((dopd::masked_few_kernel<D, KV8, TREE>), grid, block, 0, strm, a); break;
     case dopd::kMaMid: hipLaunchKernelGGL((dopd::masked_mid_kernel<D, KV8, TREE>), grid, block, 0, strm, a); break;

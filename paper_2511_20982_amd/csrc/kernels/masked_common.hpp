@@ -211,15 +211,15 @@ __device__ __forceinline__ bool ma_tiles_of(const MaskedArgs& a, const MaItem& i
 
 // The merge of the items that lie in several slices: workgroup = merge_rows packed
 // rows of the item that a slice continues, if that slice is the first to continue it;
-// thread = a 4-dim chunk of a row, the partials folded in key order:
+// thread = a 4-dim chunk of up to four rows, the partials folded in key order:
 //   M = max_s m_s,  L = sum_s 2^(m_s - M) l_s,  o = sum_s 2^(m_s - M) o~_s / L.
 // Bound by the partials' bytes and the start of a kernel.
-template <int D>
-constexpr int merge_rows() { return 256 / (D / 4); }
+constexpr int merge_rows(int kind) { return ma_kind(kind).rows < 32 ? ma_kind(kind).rows : 32; }
 template <int D, int KIND>
 __global__ __launch_bounds__(256) void masked_merge_kernel(MaskedArgs a) {
   const MaKind kind = ma_kind(KIND, a.lo, a.hi);
-  constexpr int ROWS = ma_kind(KIND).rows, kGroup = merge_rows<D>(), CH = D / 4;
+  constexpr int ROWS = ma_kind(KIND).rows, kGroup = merge_rows(KIND), CH = D / 4;
+  constexpr int STEP = 256 / CH, R = kGroup / STEP;  // rows that the threads cover at once; rows of a thread
   const int g = (int)a.by_g.d;
   const int slice = 1 + (int)blockIdx.x / (ROWS / kGroup), group = (int)blockIdx.x % (ROWS / kGroup);
   MaItem it;
@@ -239,34 +239,54 @@ __global__ __launch_bounds__(256) void masked_merge_kernel(MaskedArgs a) {
   const int b0 = ma_slice_of(first + a.seg, a.slices), b1 = ma_slice_of(first + a.seg + tiles - 1, a.slices);
   if (b0 == b1 || slice != b0 + 1) return;
   const int slot0 = 2 * b0 + (ma_slice_begin(b0, a.slices) >= first ? 0 : 1);
-  const int row = kGroup * group + (int)threadIdx.x / CH, e0 = 4 * ((int)threadIdx.x % CH);
-  if (row < live) {
-    float M = -INFINITY, L = 0.f;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int b = b0; b <= b1; b += 4) {  // four partials in flight
-      float2 ml[4];
-      f32x4 o[4];
+  const int row0 = kGroup * group + (int)threadIdx.x / CH, e0 = 4 * ((int)threadIdx.x % CH);
+  float M[R], L[R];
+  f32x4 acc[R];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int64_t from = (int64_t)(b + u == b0 ? slot0 : 2 * min(b + u, b1)) * ROWS + row;
-        ml[u] = *reinterpret_cast<const float2*>(a.part_ml + from * 2);
-        o[u] = *reinterpret_cast<const f32x4*>(a.part_o + from * D + e0);
-      }
+  for (int r = 0; r < R; ++r) {
+    M[r] = -INFINITY;
+    L[r] = 0.f;
+    acc[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  constexpr int P = R > 2 ? 2 : 4;  // partials in flight
+  for (int b = b0; b <= b1; b += P) {
+    float2 ml[P][R];
+    f32x4 o[P][R];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        if (b + u > b1 || ml[u].x == -INFINITY) continue;  // (a part that saw nothing of the row)
-        const float m = fmaxf(M, ml[u].x);
-        const float old = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - m), now = __builtin_amdgcn_exp2f(ml[u].x - m);
-        L = L * old + ml[u].y * now;
-        acc = acc * old + o[u] * now;
-        M = m;
+    for (int u = 0; u < P; ++u) {
+      if (b + u > b1) break;
+      const int64_t slot = b + u == b0 ? slot0 : 2 * (b + u);
+#pragma unroll
+      for (int r = 0; r < R; ++r) {  // (rows past the last: the last again)
+        const int64_t from = slot * ROWS + min(row0 + r * STEP, live - 1);
+        ml[u][r] = *reinterpret_cast<const float2*>(a.part_ml + from * 2);
+        o[u][r] = *reinterpret_cast<const f32x4*>(a.part_o + from * D + e0);
       }
     }
-    const float inv = L == 0.f ? 0.f : 1.f / L;
+#pragma unroll
+    for (int u = 0; u < P; ++u) {
+      if (b + u > b1) break;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        if (ml[u][r].x == -INFINITY) continue;  // (a part that saw nothing of the row)
+        const float m = fmaxf(M[r], ml[u][r].x);
+        const float old = M[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M[r] - m);
+        const float now = __builtin_amdgcn_exp2f(ml[u][r].x - m);
+        L[r] = L[r] * old + ml[u][r].y * now;
+        acc[r] = acc[r] * old + o[u][r] * now;
+        M[r] = m;
+      }
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int row = row0 + r * STEP;
+    if (row >= live) break;
+    const float inv = L[r] == 0.f ? 0.f : 1.f / L[r];
     const int x = x0 + row, tok = fast_quot(x, a.by_g);
     const int64_t to = (int64_t)(it.row0 + tok) * a.hq + c * g + (x - tok * g);
-    store_bf16x4(a.out, to * D + e0, acc * inv);
-    if (a.lse && e0 == 0) a.lse[to] = (M + __log2f(L)) * kLn2;
+    store_bf16x4(a.out, to * D + e0, acc[r] * inv);
+    if (a.lse && e0 == 0) a.lse[to] = (M[r] + __log2f(L[r])) * kLn2;
   }
 }
 
