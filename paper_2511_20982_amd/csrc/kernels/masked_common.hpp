@@ -96,6 +96,23 @@ __device__ __forceinline__ u32x2 keep_of(u32x2 x, uint32_t bits) {
   return x;
 }
 
+// Over the four lanes l % 16 + 0, 16, 32, 48 (on the vector unit: through LDS each of
+// the two exchanges takes some 100 cycles).
+__device__ __forceinline__ float quad_max(float x) {
+  const uint32_t b = __float_as_uint(x);
+  const auto h = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+  const uint32_t y = __float_as_uint(fmaxf(__uint_as_float(h[0]), __uint_as_float(h[1])));
+  const auto f = __builtin_amdgcn_permlane32_swap(y, y, false, false);
+  return fmaxf(__uint_as_float(f[0]), __uint_as_float(f[1]));
+}
+__device__ __forceinline__ float quad_sum(float x) {
+  const uint32_t b = __float_as_uint(x);
+  const auto h = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+  const uint32_t y = __float_as_uint(__uint_as_float(h[0]) + __uint_as_float(h[1]));
+  const auto f = __builtin_amdgcn_permlane32_swap(y, y, false, false);
+  return __uint_as_float(f[0]) + __uint_as_float(f[1]);
+}
+
 // Eight keys of a V row as a bf16 operand.
 __device__ __forceinline__ bf16x8 v_operand(u32x4 v) { return __builtin_bit_cast(bf16x8, v); }
 __device__ __forceinline__ bf16x8 v_operand(u32x2 v) {

@@ -93,8 +93,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void masked_f32_kernel(MaskedArgs a)
       odd = __ballot(bad) != 0;
     }
     float mx = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
-    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    mx = quad_max(mx);
     const float m_new = fmaxf(m, mx);
     const float m_use = m_new == -INFINITY ? 0.f : m_new;  // (no key seen so far: weights 0)
     const float alpha = expf(m - m_use);
@@ -136,8 +135,7 @@ __global__ __launch_bounds__(64 * W, 8 / W) void masked_f32_kernel(MaskedArgs a)
       compute(t1, v + W);
     }
   }
-  lsum += __shfl_xor(lsum, 16, 64);
-  lsum += __shfl_xor(lsum, 32, 64);
+  lsum = quad_sum(lsum);
   if (qg == 0) {
     s_m[w][col] = m;
     s_l[w][col] = lsum;

@@ -151,8 +151,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void masked_few_kernel(MaskedArg
         }
       }
       float mx = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
-      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+      mx = quad_max(mx);
       const float m_new = fmaxf(m_run, mx);
       const float m_use = m_new == -INFINITY ? 0.f : m_new;  // (no key seen so far: weights 0)
       const float alpha = __builtin_amdgcn_exp2f(m_run - m_use);
@@ -222,8 +221,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void masked_few_kernel(MaskedArg
   }
 
   // Row sums over the lane groups, then the merge of the waves.
-  l_run += __shfl_xor(l_run, 16, 64);
-  l_run += __shfl_xor(l_run, 32, 64);
+  l_run = quad_sum(l_run);
   if (qg == 0) {
     s_m[w][col] = m_run;
     s_l[w][col] = l_run;

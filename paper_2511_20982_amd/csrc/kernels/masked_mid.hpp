@@ -164,24 +164,33 @@ __global__ __launch_bounds__(256, 2) void masked_mid_kernel(MaskedArgs a) {
         if (!(sees >> j & 1)) s[j] = -INFINITY;
       live = any_sees<TREE>(a, base, pre, end);  // uniform
     }
-    float mx = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
-    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-    const float m_new = fmaxf(m_run, mx);
-    const float m_use = m_new == -INFINITY ? 0.f : m_new;  // (no key seen so far: weights 0)
-    const float alpha = __builtin_amdgcn_exp2f(m_run - m_use);
-    m_run = m_new;
+    // Weights are formed against the running maximum; only a sum beyond 2^20 (keys far
+    // above it, the first ones seen: inf or NaN) takes the maximum of these.
     bf16x8 p;
-    float sum = 0.f;
+    float sum;
+    auto weights = [&](float m) {
+      float part[2] = {0.f, 0.f};
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float e = __builtin_amdgcn_exp2f(s[j] - m_use);
-      sum += e;
-      p[j] = (__bf16)e;
+      for (int j = 0; j < 8; ++j) {
+        const float e = __builtin_amdgcn_exp2f(s[j] - m);
+        part[j & 1] += e;
+        p[j] = (__bf16)e;
+      }
+      sum = part[0] + part[1];
+    };
+    weights(m_run);
+    if (__ballot(!(sum <= 1048576.f))) {
+      const float mx = quad_max(fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7]))));
+      const float m_new = fmaxf(m_run, mx);
+      const float m_use = m_new == -INFINITY ? 0.f : m_new;  // (no key seen so far: weights 0)
+      const float alpha = __builtin_amdgcn_exp2f(m_run - m_use);
+      m_run = m_new;
+      l_run *= alpha;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) oacc[n] *= alpha;
+      weights(m_use);
     }
-    l_run = l_run * alpha + sum;
-#pragma unroll
-    for (int n = 0; n < NT; ++n) oacc[n] *= alpha;
+    l_run += sum;
     // V^T operand n: dims 16 n + col, keys 8 qg + 0 .. 7 (page qg / 2, half qg % 2).
     using VT = std::conditional_t<KV8, u32x2, u32x4>;
     const uint8_t* vrow = pages + (qg >> 1) * 2 * PB + PB + (KV8 ? 16 * col : 32 * col + 16 * ((qg & 1) ^ (col >> 3)));
@@ -256,8 +265,7 @@ __global__ __launch_bounds__(256, 2) void masked_mid_kernel(MaskedArgs a) {
   }
   if (!active) return;
 
-  l_run += __shfl_xor(l_run, 16, 64);
-  l_run += __shfl_xor(l_run, 32, 64);
+  l_run = quad_sum(l_run);
   const float vsc = KV8 ? a.v_scale[c] : 1.f;
   const float fac = !whole ? vsc : l_run == 0.f ? 0.f : vsc / l_run;
   const int row = 16 * w + col;
