@@ -54,7 +54,8 @@ dopd::MaPlan masked_plan(const dopd::MaKind& k, const dopd_attn_shape* s, const 
 size_t masked_ws_bytes(const dopd_attn_shape* s, const dopd::MaskRule& rule, const int32_t* cu_host,
                        const int32_t* prefix_host, int32_t nreq) {
   if (s->dtype == DOPD_FP32) return 0;
-  const dopd::MaSplit split = dopd::ma_split(rule, cu_host, prefix_host, nreq, s->num_q_heads / s->num_kv_heads);
+  const dopd::MaSplit split = dopd::ma_split(rule, cu_host, prefix_host, nreq, s->num_q_heads / s->num_kv_heads,
+                                              dopd::ma_mid(s->dtype == DOPD_FP8_E4M3, s->head_dim));
   size_t bytes = 0;
   for (int i = 0; i < 3; ++i) {
     const dopd::MaKind k = dopd::ma_kernel(split, i);
@@ -75,7 +76,9 @@ dopd_status launch_masked(const dopd::MaKind& k, const dopd::MaskedArgs& a, cons
   const dim3 grid = grid_of(p.blocks), block(256), merge((unsigned)((p.nwg - 1) * (k.rows / dopd::merge_rows(k.which))));
   switch (k.which) {
     case dopd::kMaFew: hipLaunchKernelGGL((dopd::masked_few_kernel<D, KV8, TREE>), grid, block, 0, strm, a); break;
-    case dopd::kMaMid: hipLaunchKernelGGL((dopd::masked_mid_kernel<D, KV8, TREE>), grid, block, 0, strm, a); break;
+    case dopd::kMaMid:
+      if constexpr (dopd::ma_mid(KV8, D)) hipLaunchKernelGGL((dopd::masked_mid_kernel<D, KV8, TREE>), grid, block, 0, strm, a);
+      break;
     default: hipLaunchKernelGGL((dopd::masked_rows_kernel<D, KV8, TREE>), grid, block, 0, strm, a);
   }
   const dopd_status st = launch_status();
@@ -158,7 +161,8 @@ dopd_status masked_impl(const dopd_attn_shape* s, bool kv8, const void* q, const
   }
 
   a.scale = s->softmax_scale * dopd::kLog2e;
-  const dopd::MaSplit split = dopd::ma_split(rule, cu_host, prefix_host, nreq, hq / hkv);
+  const dopd::MaSplit split = dopd::ma_split(rule, cu_host, prefix_host, nreq, hq / hkv,
+                                              dopd::ma_mid(s->dtype == DOPD_FP8_E4M3, d));
   dopd::MaPlan plans[3];
   size_t need = 0;
   for (int i = 0; i < 3; ++i) {

@@ -50,10 +50,12 @@ __global__ __launch_bounds__(kCopyThreads) void kv_copy_pages_kernel(CopyPagesAr
 // ---- accepted tokens ------------------------------------------------------------
 // Request r: position prefix[r] + i takes what position prefix[r] + path[r][i] held,
 // i < count[r], path strictly increasing (so path[i] >= i, and what a later move
-// reads no earlier one has written).  A thread moves one dim row of V (one element a
-// token) or one 16-byte chunk of K rows for all tokens of a request, kCompactTokens
-// at a time, loads before stores: it touches nothing another thread does, so the
-// moves need no barrier.  Bound by the 32-byte sectors of the V rows it touches.
+// reads no earlier one has written).  A thread moves one dim row of V or one 16-byte
+// chunk of K rows for all tokens of a request, loads before stores: it touches nothing
+// another thread does, so the moves need no barrier.  A token of V is one element of
+// each dim row, and a row is written whole: element by element, every token writes
+// parts of the same 32-byte sectors again (28 layers x 192 requests: 77 us, and 64 this way).
+// Places are uniform and come by scalar loads.  Bound by the sectors of V's rows.
 struct CompactArgs {
   char* k_pool;               // [layers][num_pages][Hkv][16][D]
   char* v_pool;               // [layers][num_pages][Hkv][D][16]
@@ -76,47 +78,71 @@ __global__ __launch_bounds__(kCompactThreads) void kv_compact_kernel(CompactArgs
   const int64_t rest = b / a.per;
   const int r = (int)(rest % a.nreq);
   const int64_t layer = rest / a.nreq;
-  const int m = min(a.count[r], a.most), pre = a.prefix[r];
-  const int32_t* pt = a.page_table + (int64_t)r * a.pt_stride;
-  const int32_t* path = a.path + (int64_t)r * a.most;
+  typedef const __attribute__((address_space(4))) int32_t* ScalarPtr;
+  const ScalarPtr count = (ScalarPtr)(uintptr_t)a.count, prefix = (ScalarPtr)(uintptr_t)a.prefix;
+  const ScalarPtr pt = (ScalarPtr)(uintptr_t)(a.page_table + (int64_t)r * a.pt_stride);
+  const ScalarPtr path = (ScalarPtr)(uintptr_t)(a.path + (int64_t)r * a.most);
+  const int m = min(count[r], a.most), pre = prefix[r];
+  if (m <= 0 || pre < 0 || pre >= kMaMaxPos) return;
   const int unit = part * kCompactThreads + (int)threadIdx.x;
   const int nv = a.hkv * D;
-  const int64_t page_elems = (int64_t)a.hkv * kPage * D;
-  const int64_t base = layer * a.num_pages * page_elems;
+  const int64_t page_elems = (int64_t)a.hkv * kPage * D, base = layer * a.num_pages * page_elems;
 
-  // Page and slot of a position; a negative page where the table has none.
+  // Page of a position; a negative one where the table has none.
   auto page_of = [&](int pos) {
-    if (pos < 0 || pos / kPage >= a.pt_stride) return -1;
+    if (pos / kPage >= a.pt_stride) return -1;
     const int p = pt[pos / kPage];
     return p < a.num_pages ? p : -1;
   };
-  auto move = [&](auto* at, int slot_elems) {  // `at`: this thread's element of page 0, slot 0
-    using E = std::remove_reference_t<decltype(*at)>;
-    constexpr int ratio = sizeof(E) / sizeof(T);
+  // Where token i comes from: its position, and its page (-1: it stays, or has no path).
+  auto source = [&](int i, int& pos) {
+    const int from = path[i];
+    if (from <= i || from >= kMaMaxPos) return -1;
+    pos = pre + from;
+    return page_of(pos);
+  };
+  if (unit < nv) {
+    T* at = reinterpret_cast<T*>(a.v_pool) + base + (int64_t)unit * kPage;  // this thread's row of page 0
+    for (int t = pre / kPage; t <= (pre + m - 1) / kPage; ++t) {
+      const int pd = page_of(t * kPage);
+      if (pd < 0) continue;
+      typedef T Row __attribute__((ext_vector_type(kPage)));
+      Row* to = reinterpret_cast<Row*>(at + pd * page_elems);
+      Row x = *to;
+      bool any = false;
+#pragma unroll
+      for (int s = 0; s < kPage; ++s) {
+        const int i = t * kPage + s - pre;
+        if (i < 0 || i >= m) continue;
+        int pos = 0;
+        const int ps = source(i, pos);
+        if (ps < 0) continue;
+        x[s] = at[ps * page_elems + pos % kPage];
+        any = true;
+      }
+      if (any) *to = x;
+    }
+  } else if (unit < nv + a.hkv * CPR) {
+    const int k = unit - nv, h = k / CPR, q = k % CPR;
+    u32x4* at = reinterpret_cast<u32x4*>(reinterpret_cast<T*>(a.k_pool) + base + (int64_t)h * kPage * D) + q;
+    constexpr int ratio = 16 / sizeof(T);
     for (int i0 = 0; i0 < m; i0 += kCompactTokens) {
-      E x[kCompactTokens];
-      E* to[kCompactTokens];
+      u32x4 x[kCompactTokens];
+      int64_t to[kCompactTokens];
 #pragma unroll
       for (int u = 0; u < kCompactTokens; ++u) {
-        to[u] = nullptr;
+        to[u] = -1;
         if (i0 + u >= m) continue;
-        const int from = path[i0 + u];
-        if (from <= i0 + u || from >= kMaMaxPos || pre >= kMaMaxPos) continue;  // (in place, or no path)
-        const int ps = page_of(pre + from), pd = page_of(pre + i0 + u);
+        int pos = 0;
+        const int ps = source(i0 + u, pos), pd = page_of(pre + i0 + u);
         if (ps < 0 || pd < 0) continue;
-        x[u] = at[(ps * page_elems + ((pre + from) % kPage) * slot_elems) / ratio];
-        to[u] = at + (pd * page_elems + ((pre + i0 + u) % kPage) * slot_elems) / ratio;
+        x[u] = at[(ps * page_elems + (pos % kPage) * D) / ratio];
+        to[u] = (pd * page_elems + ((pre + i0 + u) % kPage) * D) / ratio;
       }
 #pragma unroll
       for (int u = 0; u < kCompactTokens; ++u)
-        if (to[u]) *to[u] = x[u];
+        if (to[u] >= 0) at[to[u]] = x[u];
     }
-  };
-  if (unit < nv) {
-    move(reinterpret_cast<T*>(a.v_pool) + base + (int64_t)unit * kPage, 1);
-  } else if (unit < nv + a.hkv * CPR) {
-    const int k = unit - nv, h = k / CPR, q = k % CPR;
-    move(reinterpret_cast<u32x4*>(reinterpret_cast<T*>(a.k_pool) + base + (int64_t)h * kPage * D) + q, D);
   }
 }
 

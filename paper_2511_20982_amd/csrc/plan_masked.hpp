@@ -193,10 +193,17 @@ inline MaPlan ma_plan(const MaskRule& m, const MaKind& k, const int32_t* cu, con
 // The kernels of a call: those whose requests carry a fair share of its tiles.  A
 // class of fewer rows whose share is small goes with the next (whose kernel can take
 // it, less efficiently) rather than to a launch of its own behind the others.
+// mid: is the kernel of up to 64 rows the better one for them?  Its waves read and
+// convert every tile for 16 rows each, the many-row kernel's for 32.  bf16 at d = 128:
+// 115 us against 129 (48 rows over 3000 keys, 32 requests x 8 KV heads), d = 64 106
+// against 106; E4M3, where that work counts, at d = 128 138 us against 117 (24 rows, 64
+// requests), 94 against 90 (64 rows), at d = 64, whose tiles are too small for the
+// many-row kernel's steps, 86 against 97 (32 rows).
+constexpr bool ma_mid(bool fp8, int d) { return !(fp8 && d == 128); }
 struct MaSplit {
   int hi16, hi64;  // the first kernel takes rows up to hi16, the second up to hi64, the third the rest
 };
-inline MaSplit ma_split(const MaskRule& m, const int32_t* cu, const int32_t* pre, int nreq, int g) {
+inline MaSplit ma_split(const MaskRule& m, const int32_t* cu, const int32_t* pre, int nreq, int g, bool mid) {
   double tiles[3] = {0, 0, 0};  // of 32 keys
   for (int r = 0; r < nreq; ++r) {
     const int n = cu[r + 1] - cu[r];
@@ -211,7 +218,7 @@ inline MaSplit ma_split(const MaskRule& m, const int32_t* cu, const int32_t* pre
     s.hi16 = 0;
     tiles[1] += tiles[0];
   }
-  if (tiles[1] < kShare * tiles[2]) s.hi64 = s.hi16;
+  if (!mid || tiles[1] < kShare * tiles[2]) s.hi64 = s.hi16;
   return s;
 }
 // Kernel i (0, 1, 2) of a call.
