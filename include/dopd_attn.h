@@ -597,8 +597,9 @@ size_t dopd_tree_workspace_size(const dopd_attn_shape* shape, const int32_t* cu_
  * K and V that position prefix_lens[r] + accepted[r * max_accepted + i] held before
  * the call, for i < num_accepted[r].  A row of accepted is strictly increasing (a
  * path of a tree whose drafts come after their parents), so accepted[i] >= i.  Pure
- * bit copy in place; every other slot is left untouched (what the drafts held
- * behind the accepted ones stays, dead).
+ * bit copy in place; every other slot keeps what it holds (what the drafts held
+ * behind the accepted ones stays, dead).  V rows are written whole: until the call is
+ * done, nothing else may write to a page that it moves a token into.
  *   k_pool/v_pool: with a leading layer dimension, as in dopd_kv_pack_for_handoff;
  *     requests do not share the pages that are written (dopd_kv_copy_pages first).
  *   prefix_lens, accepted [num_reqs][max_accepted], num_accepted [num_reqs] are

@@ -45,7 +45,7 @@ dopd::MaskRule tree_rule() { return dopd::MaskRule{1, 0, 0}; }
 
 dopd::MaPlan masked_plan(const dopd::MaKind& k, const dopd_attn_shape* s, const dopd::MaskRule& rule,
                          const int32_t* cu_host, const int32_t* prefix_host, int32_t nreq) {
-  const dopd::MaCosts cost = k.which == dopd::kMaMany ? dopd::MaCosts{6, 12, 6}
+  const dopd::MaCosts cost = k.which == dopd::kMaMany ? dopd::MaCosts{20, 12, 6}
                                                       : dopd::MaCosts{s->dtype == DOPD_FP8_E4M3 ? 12 : 8, 16, 4};
   const int g = s->num_q_heads / s->num_kv_heads;
   return dopd::ma_plan(rule, k, cu_host, prefix_host, nreq, g, s->num_kv_heads, machine_shape(), cost);
