@@ -2,8 +2,8 @@
 // larger trees), bf16 in / fp32 accumulate, over bf16 or E4M3 pages.
 //
 // Workgroup = 4 waves = an item of 128 packed rows of one (request, KV head), 32 rows
-// a wave, or a slice of the call's items; two workgroups share a CU.  Packing the g query heads of a
-// KV head into the rows lets 128 / g tokens share a tile, so that a window's
+// a wave, or a slice of the call's items; two workgroups share a CU.  Packing the g query
+// heads of a KV head into the rows lets 128 / g tokens share a tile, so that a window's
 // ragged ends take few masked tiles and a small tree fills the matrix units.  Per
 // visited tile of 32 keys and wave
 //   S^T[32 keys][32] = K[32][d] . Q^T[d][32]        d / 16 v_mfma_f32_32x32x16_bf16
@@ -266,10 +266,13 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
   // i + 1, the weights of tile i, and the product of the weights of tile i - 1 with V.
   // It ends when what step i + 1 reads has landed: this wave's loads of the three steps
   // before may be in flight then.
-  int pid_k = page_of(v0), pid_k1 = pid_k, pid_v = pid_k;
+  int id[6];  // (all at once: one after the other, an item began with five trips to memory)
+#pragma unroll
+  for (int i = 0; i < 6; ++i) id[i] = page_of(v0 + i);
+  int pid_k = id[5], pid_k1 = id[4], pid_v = id[3];
   auto issue = [&](int v, uint16_t* st) {
     const int next = page_of(v + 6);
-    load(st, pid_k, v + 5 < v1, pid_v, v + 3 >= v0 && v + 3 < v1);
+    load(st, pid_k, v + 5 < v1, pid_v, v + 3 < v1);
     pid_v = pid_k1;
     pid_k1 = pid_k;
     pid_k = next;
@@ -281,11 +284,11 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
   };
   for (int i = (int)threadIdx.x; i < TE / 8; i += kRowsThreads)  // (step 0: weights 0 and no V)
     reinterpret_cast<u32x4*>(st0 + TE)[i] = u32x4{0, 0, 0, 0};
-  issue(v0 - 5, st4);
-  issue(v0 - 4, st0);
-  issue(v0 - 3, st1);
-  issue(v0 - 2, st2);
-  issue(v0 - 1, st3);
+  load(st4, id[0], true, id[0], false);
+  load(st0, id[1], v0 + 1 < v1, id[0], false);
+  load(st1, id[2], v0 + 2 < v1, id[0], true);
+  load(st2, id[3], v0 + 3 < v1, id[1], v0 + 1 < v1);
+  load(st3, id[4], v0 + 4 < v1, id[2], v0 + 2 < v1);
   finish(v0 - 1, st0);
   f32x16 sa, sb;  // S^T of two consecutive tiles
   qk(st4, sa);
