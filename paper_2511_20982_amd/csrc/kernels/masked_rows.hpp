@@ -13,7 +13,9 @@
 // flight: the time such a load takes under traffic is several times a tile's work.
 // (Double-buffered 64-key tiles: 16 chunks of 512 x 32 heads, window 1024, 243 us;
 // without their loads 168, without the work 158.)
-// Bound by the matrix units and the softmax for wide items, by HBM for few rows.
+// Bound by the matrix units and the softmax for wide items (two chunks of 1021 over
+// E4M3, window 4001: 285 us, 940 TFLOP/s; those 16 chunks: 203 us, 602 TFLOP/s of
+// visible keys, their loads alone 134, their work alone 157), by HBM for few rows.
 #pragma once
 #include "masked_few.hpp"
 
