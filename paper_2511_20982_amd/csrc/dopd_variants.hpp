@@ -54,7 +54,7 @@ dopd::MaPlan masked_plan(const dopd::MaKind& k, const dopd_attn_shape* s, const 
 size_t masked_ws_bytes(const dopd_attn_shape* s, const dopd::MaskRule& rule, const int32_t* cu_host,
                        const int32_t* prefix_host, int32_t nreq) {
   if (s->dtype == DOPD_FP32) return 0;
-  const dopd::MaSplit split = dopd::ma_split(rule, cu_host, prefix_host, nreq, s->num_q_heads / s->num_kv_heads,
+  const dopd::MaSplit split = dopd::ma_split(rule, cu_host, prefix_host, nreq, s->num_q_heads / s->num_kv_heads, s->num_kv_heads,
                                               dopd::ma_mid(s->dtype == DOPD_FP8_E4M3, s->head_dim));
   size_t bytes = 0;
   for (int i = 0; i < 3; ++i) {
@@ -161,7 +161,7 @@ dopd_status masked_impl(const dopd_attn_shape* s, bool kv8, const void* q, const
   }
 
   a.scale = s->softmax_scale * dopd::kLog2e;
-  const dopd::MaSplit split = dopd::ma_split(rule, cu_host, prefix_host, nreq, hq / hkv,
+  const dopd::MaSplit split = dopd::ma_split(rule, cu_host, prefix_host, nreq, hq / hkv, hkv,
                                               dopd::ma_mid(s->dtype == DOPD_FP8_E4M3, d));
   dopd::MaPlan plans[3];
   size_t need = 0;

@@ -190,9 +190,8 @@ inline MaPlan ma_plan(const MaskRule& m, const MaKind& k, const int32_t* cu, con
   return p;
 }
 
-// The kernels of a call: those whose requests carry a fair share of its tiles.  A
-// class of fewer rows whose share is small goes with the next (whose kernel can take
-// it, less efficiently) rather than to a launch of its own behind the others.
+// The kernels of a call.  A class of fewer rows can go with the next (whose kernel
+// takes it, less efficiently) rather than to a launch of its own behind the others.
 // mid: is the kernel of up to 64 rows the better one for them?  Its waves read and
 // convert every tile for 16 rows each, the many-row kernel's for 32.  bf16 at d = 128:
 // 115 us against 129 (48 rows over 3000 keys, 32 requests x 8 KV heads), d = 64 106
@@ -203,7 +202,7 @@ constexpr bool ma_mid(bool fp8, int d) { return !(fp8 && d == 128); }
 struct MaSplit {
   int hi16, hi64;  // the first kernel takes rows up to hi16, the second up to hi64, the third the rest
 };
-inline MaSplit ma_split(const MaskRule& m, const int32_t* cu, const int32_t* pre, int nreq, int g, bool mid) {
+inline MaSplit ma_split(const MaskRule& m, const int32_t* cu, const int32_t* pre, int nreq, int g, int hkv, bool mid) {
   double tiles[3] = {0, 0, 0};  // of 32 keys
   for (int r = 0; r < nreq; ++r) {
     const int n = cu[r + 1] - cu[r];
@@ -212,13 +211,20 @@ inline MaSplit ma_split(const MaskRule& m, const int32_t* cu, const int32_t* pre
     const int c = rows <= 16 ? 0 : rows <= 64 ? 1 : 2;
     tiles[c] += ma_most_tiles(m, pre[r], n, g, ma_kind(kMaMid)) * (c == 2 ? (double)ma_row_tiles(n, g, 128) : 1.);
   }
-  constexpr double kShare = 0.25;
+  // Few-row requests beside those of the middle kernel, which reads a tile once for up
+  // to 64 rows, go with them unless they are most of the work: 32 trees of 8 drafts and
+  // 32 decodes 97 us against 135 as two launches, 64 decodes 175 against 172.  The
+  // many-row kernel takes a class whose tiles are few: 8 a workgroup or less (2 chunks of
+  // 256 and 8 decodes over 1000 keys 70 us against 83; 8 chunks and 16 decodes over 2000
+  // keys, 64/8 heads, 354 against 319).
+  const double few = 4096. / hkv;
   MaSplit s{16, 64};
-  if (tiles[0] < kShare * (tiles[1] + tiles[2])) {
+  const bool beside = mid && tiles[1] > 0;
+  if (tiles[1] + tiles[2] > 0 && tiles[0] < (beside ? 2 * tiles[1] : few)) {
     s.hi16 = 0;
     tiles[1] += tiles[0];
   }
-  if (!mid || tiles[1] < kShare * tiles[2]) s.hi64 = s.hi16;
+  if (!mid || (tiles[2] > 0 && tiles[1] < few)) s.hi64 = s.hi16;
   return s;
 }
 // Kernel i (0, 1, 2) of a call.

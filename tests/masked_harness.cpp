@@ -190,7 +190,7 @@ int main(int argc, char** argv) {
       pre.push_back(pick(0, 4) ? log(0, 900) : pick(0, 100000));
     }
     const MaCosts cost{pick(0, 12), pick(0, 20), pick(1, 6)};
-    const MaSplit split = ma_split(m, cu.data(), pre.data(), reqs, g, pick(0, 1) != 0);
+    const MaSplit split = ma_split(m, cu.data(), pre.data(), reqs, g, hkv, pick(0, 1) != 0);
     std::vector<int> taken(reqs, 0);
     for (int j = 0; j < 4; ++j) {
       const MaKind k = j < 3 ? ma_kernel(split, j) : ma_kind(kMaF32);
