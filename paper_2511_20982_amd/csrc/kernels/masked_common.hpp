@@ -285,7 +285,9 @@ __global__ __launch_bounds__(256) void masked_merge_kernel(MaskedArgs a) {
       if (b + u > b1) break;
 #pragma unroll
       for (int r = 0; r < R; ++r) {
-        if (ml[u][r].x == -INFINITY) continue;  // (a part that saw nothing of the row)
+        // A part that saw nothing of the row.  (One whose scores are all NaN has the same
+        // maximum, and a sum of NaN: 0 times that makes the row NaN, in any order of parts.)
+        if (ml[u][r].x == -INFINITY && ml[u][r].y == 0.f) continue;
         const float m = fmaxf(M[r], ml[u][r].x);
         const float old = M[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M[r] - m);
         const float now = __builtin_amdgcn_exp2f(ml[u][r].x - m);
