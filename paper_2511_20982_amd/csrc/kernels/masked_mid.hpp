@@ -166,7 +166,8 @@ __global__ __launch_bounds__(256, 2) void masked_mid_kernel(MaskedArgs a) {
       live = any_sees<TREE>(a, base, pre, end);  // uniform
     }
     // Weights are formed against the running maximum; only a sum beyond 2^20 (keys far
-    // above it, the first ones seen: inf or NaN) takes the maximum of these.
+    // above it, the first ones seen: inf or NaN) takes the maximum of these.  The careful
+    // pass always does: weights of 2^20 times large V may have been what was not finite.
     bf16x8 p;
     float sum;
     auto weights = [&](float m) {
@@ -180,7 +181,7 @@ __global__ __launch_bounds__(256, 2) void masked_mid_kernel(MaskedArgs a) {
       sum = part[0] + part[1];
     };
     weights(m_run);
-    if (__ballot(!(sum <= 1048576.f))) {
+    if (careful() || __ballot(!(sum <= 1048576.f))) {
       const float mx = quad_max(fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7]))));
       const float m_new = fmaxf(m_run, mx);
       const float m_use = m_new == -INFINITY ? 0.f : m_new;  // (no key seen so far: weights 0)

@@ -1,5 +1,6 @@
 """GPU: windowed and tree attention in calls whose contexts several workgroups share, where what one part of a row's keys
-holds has to survive the merge of the parts: NaN in Q and in K."""
+holds has to survive the merge of the parts: NaN in Q and in K; and values of V near the largest finite ones, whose sums
+stay finite as long as the weights are formed against the largest score."""
 import numpy as np
 import pytest
 
@@ -70,3 +71,34 @@ def test_nan_in_all_keys_of_some_parts(new, dtype, backwards):
             dev["k"][int(page), 0] = bits
         out, lse = U.run(c, how, dev)
         assert np.isnan(out).all() and np.isnan(lse).all(), f"{new} {dtype}: NaN in tile {t} and those before it in turn"
+
+
+def steep(new, prefix, value, low):
+    """Rows of a KV head with g = 8 whose scores are 0 in the 32-key tiles `low` and 9.6875 (14 octaves up) in the others,
+    over V of +-value .. 2 value."""
+    n = len(prefix)
+    c = U.case(1640, prefix, [new] * n, 8, 1, 128, "bf16")
+    c["scale"] = 1.0
+    bits = lambda x: (np.asarray(x, np.float32).view(np.uint32) >> 16).astype(np.uint16)  # noqa: E731
+    c["q"][:] = 0
+    c["q"][:, :, 0] = bits(1.0)
+    rng = np.random.default_rng(5)
+    for r, pre in enumerate(prefix):
+        at = np.arange(pre + new)
+        page, slot = c["pt"][r, at // 16], at % 16
+        k = np.zeros((len(at), 1, 128), np.float32)
+        k[:, 0, 0] = np.where(np.isin(at // 32, low), 0.0, 9.6875)
+        v = rng.choice([-1.0, 1.0], (len(at), 1, 128)) * (1 + rng.random((len(at), 1, 128)) * 0.99) * value
+        c["k"][page, :, slot, :] = bits(k)
+        c["v"][page, :, :, slot] = bits(v)
+    return c
+
+
+@pytest.mark.parametrize("new", SIZES)
+def test_large_values_under_rising_scores(new):
+    """Items that run whole: 2^14 times the weights of the first tile, times V of 2^112, times 130 keys are beyond fp32."""
+    c = steep(new, [130, 75], 2.0 ** 112, [0])
+    assert A.dopd_window_workspace_size(U.shape_of(c), c["cu"], c["prefix"], 2, 10 ** 6, 0) == 256
+    ref = U.window_reference(c, 10 ** 6, 0)
+    assert np.isfinite(ref[0]).all()
+    U.check(U.run(c, ("window", 10 ** 6, 0)), ref, c, f"V of 2^112, {new}")
