@@ -226,6 +226,18 @@ __device__ __forceinline__ bool ma_tiles_of(const MaskedArgs& a, const MaItem& i
   return v0 == 0 && v1 == n;
 }
 
+// A part's sum may hold weights far above 1 where they were formed against a maximum that
+// stayed behind: its binary exponent moves from the sum (which becomes 0.5 .. 1; 0, inf and
+// NaN stay) and the part's O, whose factor is returned, to the maximum.  Both factors are
+// powers of two, so only the maximum's sum rounds; parts of large V then add up as they do
+// under their true maxima.
+__device__ __forceinline__ float part_to_unit_sum(float& m, float& l) {
+  const int e = __builtin_amdgcn_frexp_expf(l);
+  m += (float)e;
+  l = __builtin_amdgcn_ldexpf(l, -e);
+  return __builtin_amdgcn_ldexpf(1.f, -e);
+}
+
 // The merge of the items that lie in several slices: workgroup = merge_rows packed
 // rows of the item that a slice continues, if that slice is the first to continue it;
 // thread = a 4-dim chunk of up to four rows, the partials folded in key order:

@@ -269,7 +269,7 @@ __global__ __launch_bounds__(256, 2) void masked_mid_kernel(MaskedArgs a) {
 
   l_run = quad_sum(l_run);
   const float vsc = KV8 ? a.v_scale[c] : 1.f;
-  const float fac = !whole ? vsc : l_run == 0.f ? 0.f : vsc / l_run;
+  const float fac = !whole ? vsc * part_to_unit_sum(m_run, l_run) : l_run == 0.f ? 0.f : vsc / l_run;
   const int row = 16 * w + col;
   if (row >= rows) return;
 #pragma unroll

@@ -404,10 +404,11 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
 
   // Stages become the waves' output staging, 16-byte chunks swizzled by row.
   if (active) {
-  const float L = l_run + __shfl_xor(l_run, 32, 64);
+  float L = l_run + __shfl_xor(l_run, 32, 64);
   const float vsc = KV8 ? a.v_scale[c] : 1.f;
   const bool mine = xw + (l & 31) < rows;
   if (!whole) {
+    const float fac = vsc * part_to_unit_sum(m_run, L);
     const int64_t at = (int64_t)it.slot * ROWS + 32 * w + (l & 31);
     if (mine) {
       float* po = a.part_o + at * D + 4 * hi;
@@ -416,7 +417,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
 #pragma unroll
         for (int q = 0; q < 4; ++q)
           *reinterpret_cast<f32x4*>(po + 32 * et + 8 * q) =
-              f32x4{oacc[et][4 * q], oacc[et][4 * q + 1], oacc[et][4 * q + 2], oacc[et][4 * q + 3]} * vsc;
+              f32x4{oacc[et][4 * q], oacc[et][4 * q + 1], oacc[et][4 * q + 2], oacc[et][4 * q + 3]} * fac;
       if (hi == 0) *reinterpret_cast<float2*>(a.part_ml + at * 2) = float2{m_run, L};
     }
   } else {

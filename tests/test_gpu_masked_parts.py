@@ -75,7 +75,7 @@ def test_nan_in_all_keys_of_some_parts(new, dtype, backwards):
 
 def steep(new, prefix, value, low):
     """Rows of a KV head with g = 8 whose scores are 0 in the 32-key tiles `low` and 9.6875 (14 octaves up) in the others,
-    over V of +-value .. 2 value."""
+    over V of value .. 2 value, of one sign in each dim."""
     n = len(prefix)
     c = U.case(1640, prefix, [new] * n, 8, 1, 128, "bf16")
     c["scale"] = 1.0
@@ -88,7 +88,7 @@ def steep(new, prefix, value, low):
         page, slot = c["pt"][r, at // 16], at % 16
         k = np.zeros((len(at), 1, 128), np.float32)
         k[:, 0, 0] = np.where(np.isin(at // 32, low), 0.0, 9.6875)
-        v = rng.choice([-1.0, 1.0], (len(at), 1, 128)) * (1 + rng.random((len(at), 1, 128)) * 0.99) * value
+        v = np.where(np.arange(128) % 3, 1.0, -1.0) * (1 + rng.random((len(at), 1, 128)) * 0.99) * value
         c["k"][page, :, slot, :] = bits(k)
         c["v"][page, :, :, slot] = bits(v)
     return c
@@ -102,3 +102,20 @@ def test_large_values_under_rising_scores(new):
     ref = U.window_reference(c, 10 ** 6, 0)
     assert np.isfinite(ref[0]).all()
     U.check(U.run(c, ("window", 10 ** 6, 0)), ref, c, f"V of 2^112, {new}")
+
+
+@pytest.mark.parametrize("new", [1, 6, 16])
+def test_large_values_in_parts_that_start_low(new):
+    """Every part's first tile is far below the rest of it, so that its weights (formed against the first tile) are up to
+    2^14: V of 2^105 leaves each part finite, and the sum of the parts as they stand beyond fp32."""
+    prefix, rows, seg = 3000, {1: 16, 6: 64, 16: 128}[new], {1: 8, 6: 8, 16: 20}[new]
+    c = steep(new, [prefix], 1.0, [0])
+    size = A.dopd_window_workspace_size(U.shape_of(c), c["cu"], c["prefix"], 1, 10 ** 6, 0)
+    parts = size // (2 * rows * (128 + 2) * 4)
+    units = seg + (prefix + new + 31) // 32
+    first = [max(0, i * (units // parts) + min(i, units % parts) - seg) for i in range(parts)]
+    assert parts >= 8 and len(set(first)) >= 8
+    c = steep(new, [prefix], 2.0 ** 105, first)
+    ref = U.window_reference(c, 10 ** 6, 0)
+    assert np.isfinite(ref[0]).all()
+    U.check(U.run(c, ("window", 10 ** 6, 0)), ref, c, f"V of 2^105 in {parts} parts, {new}")
