@@ -55,7 +55,7 @@ size_t masked_ws_bytes(const dopd_attn_shape* s, const dopd::MaskRule& rule, con
                        const int32_t* prefix_host, int32_t nreq) {
   if (s->dtype == DOPD_FP32) return 0;
   const dopd::MaSplit split = dopd::ma_split(rule, cu_host, prefix_host, nreq, s->num_q_heads / s->num_kv_heads, s->num_kv_heads,
-                                              dopd::ma_mid(s->dtype == DOPD_FP8_E4M3, s->head_dim));
+                                              dopd::ma_mid(s->dtype == DOPD_FP8_E4M3, s->head_dim), machine_shape());
   size_t bytes = 0;
   for (int i = 0; i < 3; ++i) {
     const dopd::MaKind k = dopd::ma_kernel(split, i);
@@ -162,7 +162,7 @@ dopd_status masked_impl(const dopd_attn_shape* s, bool kv8, const void* q, const
 
   a.scale = s->softmax_scale * dopd::kLog2e;
   const dopd::MaSplit split = dopd::ma_split(rule, cu_host, prefix_host, nreq, hq / hkv, hkv,
-                                              dopd::ma_mid(s->dtype == DOPD_FP8_E4M3, d));
+                                              dopd::ma_mid(s->dtype == DOPD_FP8_E4M3, d), machine_shape());
   dopd::MaPlan plans[3];
   size_t need = 0;
   for (int i = 0; i < 3; ++i) {

@@ -202,7 +202,8 @@ constexpr bool ma_mid(bool fp8, int d) { return !(fp8 && d == 128); }
 struct MaSplit {
   int hi16, hi64;  // the first kernel takes rows up to hi16, the second up to hi64, the third the rest
 };
-inline MaSplit ma_split(const MaskRule& m, const int32_t* cu, const int32_t* pre, int nreq, int g, int hkv, bool mid) {
+inline MaSplit ma_split(const MaskRule& m, const int32_t* cu, const int32_t* pre, int nreq, int g, int hkv, bool mid,
+                        const MachineShape& mach = kDefaultMachine) {
   double tiles[3] = {0, 0, 0};  // of 32 keys
   for (int r = 0; r < nreq; ++r) {
     const int n = cu[r + 1] - cu[r];
@@ -217,7 +218,7 @@ inline MaSplit ma_split(const MaskRule& m, const int32_t* cu, const int32_t* pre
   // many-row kernel takes a class whose tiles are few: 8 a workgroup or less (2 chunks of
   // 256 and 8 decodes over 1000 keys 70 us against 83; 8 chunks and 16 decodes over 2000
   // keys, 64/8 heads, 354 against 319).
-  const double few = 4096. / hkv;
+  const double few = 8. * kWgPerCu * std::max(1, mach.cus) / hkv;
   MaSplit s{16, 64};
   const bool beside = mid && tiles[1] > 0;
   if (tiles[1] + tiles[2] > 0 && tiles[0] < (beside ? 2 * tiles[1] : few)) {
