@@ -82,8 +82,10 @@ __global__ __launch_bounds__(kCompactThreads) void kv_compact_kernel(CompactArgs
   const ScalarPtr count = (ScalarPtr)(uintptr_t)a.count, prefix = (ScalarPtr)(uintptr_t)a.prefix;
   const ScalarPtr pt = (ScalarPtr)(uintptr_t)(a.page_table + (int64_t)r * a.pt_stride);
   const ScalarPtr path = (ScalarPtr)(uintptr_t)(a.path + (int64_t)r * a.most);
-  const int m = min(count[r], a.most), pre = prefix[r];
-  if (m <= 0 || pre < 0 || pre >= kMaMaxPos) return;
+  const int pre = prefix[r];
+  if (pre < 0 || pre >= kMaMaxPos) return;
+  const int m = compact_tokens(count[r], a.most, pre, (int64_t)a.pt_stride * kPage);
+  if (m <= 0) return;
   const int unit = part * kCompactThreads + (int)threadIdx.x;
   const int nv = a.hkv * D;
   const int64_t page_elems = (int64_t)a.hkv * kPage * D, base = layer * a.num_pages * page_elems;

@@ -242,4 +242,15 @@ inline size_t ma_ws_bytes(const MaPlan& p, const MaKind& k, int d) {
   return p.nwg <= 1 ? 0 : ma_part_ml_off(p, k, d) + align256((size_t)2 * p.nwg * k.rows * 2 * sizeof(float));
 }
 
+// ---- compaction of accepted drafts ------------------------------------------------
+// Tokens of a request to look at: of the accepted ones those whose place is among the
+// `slots` of its row of the page table, and at most kMaMaxPos, so that places and loop
+// counters fit an int whatever the lists hold.
+constexpr int compact_tokens(int count, int most, int pre, int64_t slots) {
+  const int64_t room = slots - pre;
+  const int64_t m = count < most ? count : most;
+  const int64_t top = room < kMaMaxPos ? room : kMaMaxPos;
+  return (int)(m < top ? m : top);
+}
+
 }  // namespace dopd
