@@ -69,9 +69,10 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
     return (int64_t)(it.row0 + tok) * a.hq + c * g + (x - tok * g);
   };
   // Scores are c_in > 0 times K . Q: the scale's sign goes to Q, and so does a scale of
-  // 0 (inf becomes NaN there, as it would).
+  // 0 (inf becomes NaN there, as it would) or NaN (so that what a row does not see stays
+  // -inf).
   const float scale = KV8 ? a.scale * a.k_scale[c] : a.scale;
-  const float c_in = scale == 0.f ? 1.f : __builtin_fabsf(scale);
+  const float c_in = scale > 0.f || scale < 0.f ? __builtin_fabsf(scale) : 1.f;
   auto signed_q = [&](u32x4 q) {
     if (!(scale > 0.f)) {
 #pragma unroll
@@ -81,6 +82,8 @@ __global__ __launch_bounds__(kRowsThreads, 2) void masked_rows_kernel(MaskedArgs
         } else if (scale == 0.f) {
           const uint32_t lo = q[i] & 0x7f80, top = q[i] & 0x7f800000;
           q[i] = (lo == 0x7f80 ? 0x7fc0u : 0u) | (top == 0x7f800000 ? 0x7fc00000u : 0u);
+        } else {
+          q[i] = 0x7fc07fc0u;
         }
     }
     return q;

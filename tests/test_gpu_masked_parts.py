@@ -228,3 +228,17 @@ def test_scores_that_rise_around_the_limit_of_the_weights(new, prefix, rise):
     calls that run whole and in parts."""
     c = steep(new, [prefix], 1.0, [0, 3, 4, 41], rise)
     U.check(U.run(c, ("window", 10 ** 6, 0)), U.window_reference(c, 10 ** 6, 0), c, f"{new} {prefix} {rise}")
+
+
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("new", [1, 6, 40])
+def test_a_scale_of_nan_reaches_only_rows_that_see_something(new, d):
+    """A KV head with a k_scale of NaN: its rows are NaN, but those that see nothing have 0 and -inf."""
+    c = U.case(1698, [0, 300, 0], [new] * 3, 16, 2, d, "fp8")
+    c["ks"][1] = np.nan
+    mask = U.tree_masks(np.random.default_rng(2), [new] * 3, 2)
+    mask[:new:2] = 0
+    out, lse = U.run(c, ("tree", mask))
+    ref = U.tree_reference(c, mask)
+    assert np.isneginf(ref[1]).any() and np.isnan(ref[1]).any()
+    U.check((out, lse), ref, c, f"k_scale of NaN {new} {d}")
