@@ -497,14 +497,19 @@ size_t dopd_pd_step_workspace_size(const dopd_attn_shape* shape,
  *     exactly, by log-sum-exp rescaling, on the same stream).  May be null when
  *     that needs none.  Calls that overlap in time must not share it.
  *   lse (nullable): fp32 [T][Hq].
- * Requests of at most 16, at most 64 and more rows times Hq / Hkv run three kernels;
- * a call that holds several sizes launches several, or takes a few small ones into the
- * kernel of the larger.  Any Hq / Hkv.  q, out and the pools are
+ * Requests of at most 16, at most 64 and more rows times Hq / Hkv run three kernels
+ * (over E4M3 with d = 128 two: from 17 rows on the last; in fp32 one); a call that holds
+ * several sizes launches several, or takes a few small ones into the kernel of the
+ * larger.  Any Hq / Hkv.  q, out and the pools are
  * 16-byte aligned, prefix_lens[r] + n_r is at most 2^30, and
  * n_r * (Hq / Hkv)^2 < 2^32 (DOPD_ERR_INVALID_SHAPE otherwise).
  * bf16: products of bf16 operands with fp32 accumulation, weights rounded to bf16
  * before the product with V; the row sums (and lse) hold the unrounded weights.
  * fp32: fp32 throughout.
+ * Weights times V are summed in fp32 before the division by their sum: outputs are
+ * finite while |v| times the number of keys a row sees stays below 2^127.  A NaN in a
+ * row of q, or in K at a position that a row sees, makes that row NaN.  A row whose
+ * visible scores are all -inf is as one that sees nothing: out = 0 and lse = -inf.
  */
 dopd_status dopd_window_attn(const dopd_attn_shape* shape, const void* q, const void* k_pool,
                              const void* v_pool, int32_t num_pages, const int32_t* page_table,

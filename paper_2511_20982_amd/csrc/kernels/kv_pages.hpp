@@ -54,7 +54,7 @@ __global__ __launch_bounds__(kCopyThreads) void kv_copy_pages_kernel(CopyPagesAr
 // chunk of K rows for all tokens of a request, loads before stores: it touches nothing
 // another thread does, so the moves need no barrier.  A token of V is one element of
 // each dim row, and a row is written whole: element by element, every token writes
-// parts of the same 32-byte sectors again (28 layers x 192 requests: 77 us, and 64 this way).
+// parts of the same 32-byte sectors again (28 layers x 192 requests: 77 us, and 62 this way).
 // Places are uniform and come by scalar loads.  Bound by the sectors of V's rows.
 struct CompactArgs {
   char* k_pool;               // [layers][num_pages][Hkv][16][D]

@@ -214,9 +214,9 @@ inline MaSplit ma_split(const MaskRule& m, const int32_t* cu, const int32_t* pre
   }
   // Few-row requests beside those of the middle kernel, which reads a tile once for up
   // to 64 rows, go with them unless they are most of the work: 32 trees of 8 drafts and
-  // 32 decodes 97 us against 135 as two launches, 64 decodes 175 against 172.  The
+  // 32 decodes 98 us against 135 as two launches, 64 decodes 175 against 172.  The
   // many-row kernel takes a class whose tiles are few: 8 a workgroup or less (2 chunks of
-  // 256 and 8 decodes over 1000 keys 70 us against 83; 8 chunks and 16 decodes over 2000
+  // 256 and 8 decodes over 1000 keys 68 us against 83; 8 chunks and 16 decodes over 2000
   // keys, 64/8 heads, 354 against 319).
   const double few = 8. * kWgPerCu * std::max(1, mach.cus) / hkv;
   MaSplit s{16, 64};

@@ -242,3 +242,20 @@ def test_a_scale_of_nan_reaches_only_rows_that_see_something(new, d):
     ref = U.tree_reference(c, mask)
     assert np.isneginf(ref[1]).any() and np.isnan(ref[1]).any()
     U.check((out, lse), ref, c, f"k_scale of NaN {new} {d}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("prefix", [75, 3000])
+@pytest.mark.parametrize("new", [1, 6, 40])
+def test_scores_that_are_all_minus_infinity(new, prefix, dtype):
+    """Of one KV head's rows, in calls that run whole and in parts; the other head's rows are ordinary."""
+    c = U.case(1699, [prefix], [new], 16, 2, 128, dtype)
+    one, low = (np.float32(1), np.float32(-np.inf)) if dtype == "fp32" else (np.uint16(0x3F80), np.uint16(0xFF80))
+    c["q"][:, 8:, 9] = one
+    at = np.arange(prefix + new)
+    c["k"][c["pt"][0, at // 16], 1, at % 16, 9] = low
+    out, lse = U.run(c, ("window", 10 ** 6, 0))
+    assert (out[:, 8:] == 0).all() and np.isneginf(lse[:, 8:]).all()
+    want, want_lse, weighted, products = U.window_reference(c, 10 ** 6, 0)
+    first = lambda x: np.ascontiguousarray(x[:, :8])  # noqa: E731
+    U.check((first(out), first(lse)), tuple(map(first, (want, want_lse, weighted, products))), c, f"{new} {prefix} {dtype}")
